@@ -47,7 +47,8 @@ typedef enum {
     NNV_KIND_COUNT = 6
 } nnv_kind;
 
-typedef enum { NNV_F32 = 0, NNV_F16 = 1 } nnv_dtype;
+/* NNV_BF16 is a storage type of the serving operators (end of this file); a convolution refuses it. */
+typedef enum { NNV_F32 = 0, NNV_F16 = 1, NNV_BF16 = 2 } nnv_dtype;
 
 typedef enum {
     NNV_OK = 0,
@@ -283,6 +284,126 @@ int nnv_cache_write(const char *path, const nnv_conv_desc *desc, nnv_kind kind, 
  * Errors: NULL, BAD_DESC, ARG, UNSUPPORTED, ALIGN, HIP, IO, CACHE. */
 int nnv_cache_read(const char *path, const nnv_conv_desc *desc, nnv_kind kind, void *w_tx, int verify,
                    void *hip_stream, nnv_cache_io *io);
+
+/* ---- operators of a language model's layer as a serving program runs it: the same division into weight
+ * transformation and execution for products whose weights are held in 8 bits, and, for its attention, the
+ * plan of a step, norms and rotations of queries and keys, a cache held in 4 bits and attention over
+ * that cache.  As everywhere here: device pointers, the caller's buffers, work enqueued on the given stream,
+ * no allocation, no state kept between calls.  Tensors are 16-byte aligned; int32 arrays and bias 4-byte,
+ * int64 arrays 8-byte aligned.  Every call may be captured into a HIP graph.  Results are the same from
+ * run to run, bit for bit.
+ *
+ * 8 bits: e4m3 codes (largest 448), value = 2^e * code, one e for 128 consecutive inputs of a row of x and one for
+ * each 128 x 128 block of the weights: the smallest e (>= -126) with amax <= 448 * 2^e, so that nothing saturates.
+ * 4 bits: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), one e for 32 consecutive values of a head: the
+ * smallest e (>= -126) with amax < 7 * 2^e, so that nothing is clipped by more than a rounding; at most 13 where dtype is
+ * float16 and 125 in bfloat16 (magnitudes above 6 * 2^13 = 49152 and 6 * 2^125 are held as those).  Both round to nearest, ties to the even code.  The scales are powers of two because
+ * the matrix cores and the conversion instructions apply those themselves, and because dividing by one is exact. */
+
+typedef struct {
+    int32_t n, k;       /* y = x W^T: W is n x k */
+    int32_t x_dtype;    /* nnv_dtype of x */
+    int32_t y_dtype;    /* nnv_dtype of y */
+    int32_t raw_dtype;  /* nnv_dtype of the raw weights */
+} nnv_linear_desc;
+
+/* Bytes of the transformed weights (0 if the descriptor is invalid): one per weight of blocks of 128 x 128, and the scales. */
+size_t nnv_linear_transformed_bytes(const nnv_linear_desc *desc);
+
+/* Bytes of scratch of nnv_linear_forward over m rows (0 if invalid): x in 8 bits with its scales, and where the
+ * reduction of a few rows is split, partial sums. */
+size_t nnv_linear_workspace_bytes(const nnv_linear_desc *desc, int m);
+
+/* Raw weights (n x k of desc.raw_dtype, rows of k) -> 8-bit codes in the order that the matrix instructions read, and scales.
+ *   w_tx : nnv_linear_transformed_bytes(desc) bytes, fully overwritten
+ * A block that holds a NaN or an infinity yields NaN wherever its codes of these enter a product.
+ * Errors: NULL, BAD_DESC, ALIGN, HIP. */
+int nnv_linear_transform_weights(const nnv_linear_desc *desc, const void *w_raw, void *w_tx, void *hip_stream);
+
+/* y = x W^T + bias over m rows (0: nothing is done): x is rounded to 8 bits as above, products and sums are float32 on the
+ * matrix cores, rounded once to desc.y_dtype.
+ *   x : m rows of k elements, ldx >= k elements apart (any ldx; rows that are 16-byte aligned read faster)
+ *   y : m rows of n elements, ldy >= n elements apart;  bias : n float32, or NULL
+ *   workspace : >= nnv_linear_workspace_bytes(desc, m) bytes, whatever its contents
+ * A row of x that holds a NaN or an infinity yields NaN in that row of y.
+ * Errors: NULL, BAD_DESC, ARG, WORKSPACE, ALIGN, HIP. */
+int nnv_linear_forward(const nnv_linear_desc *desc, int m, const void *x, int64_t ldx, const void *w_tx, const float *bias, void *y,
+                       int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* An attention layer over a cache of blocks.  Fields that a call does not name are not looked at beyond their range. */
+typedef struct {
+    int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads, at most 1024 */
+    int32_t head_dim;           /* 64, 128 or 256 */
+    int32_t block_tokens;       /* tokens of a cache block: 16, 32, 64, 128 or 256 */
+    int32_t blocks;             /* blocks of the cache */
+    int32_t table_blocks;       /* columns of the block table: the most blocks of one request */
+    int32_t rotary_dim;         /* leading values of a head that are rotated: even, 0 to head_dim */
+    int32_t rotary_interleaved; /* 1: neighbours (2i, 2i + 1) turn together; 0: i and i + rotary_dim / 2 */
+    int32_t positions;          /* rows of the rotation table (not looked at where rotary_dim is 0) */
+    int32_t window;             /* a row sees this many tokens up to its own; 0: all */
+    int32_t sinks;              /* and, behind the window, the first so many tokens of the request */
+    int32_t dtype;              /* NNV_F16 or NNV_BF16: queries, keys, values, outputs */
+    float scale;                /* factor of the scores */
+    float eps;                  /* of the norms */
+} nnv_attention_desc;
+
+/* Bytes of the cache (0 if the descriptor is invalid): blocks x kv_heads x block_tokens x head_dim x 17/16, keys and values.  A
+ * slot is a token's place in it, block * block_tokens + place in the block.  Any contents are safe to read. */
+size_t nnv_kv_cache_bytes(const nnv_attention_desc *desc);
+
+/* The plan of a step: which cache blocks the new tokens of every request get, and where each row of the step lies.
+ * The step's rows are the new tokens of request 0, then of request 1, and so on.
+ *   held, fresh : n_requests int32, tokens already in the cache and new ones (0 and more; rows of a negative count are none)
+ *   free_blocks, free_count : int32 block numbers, and (one int32 on the device) how many of them there are, at most
+ *       desc.blocks; new blocks are taken from the end of the list
+ *   block_table : n_requests x table_blocks int32, updated in place: entries [ceil(held / block_tokens),
+ *       ceil((held + fresh) / block_tokens)) of an admitted request are written
+ *   starts : n_requests + 1 int32, row of each request's first new token, capped at n_rows
+ *   lengths : n_requests int32, tokens of each request in the cache after the step
+ *   positions, slots : n_rows int32 and int64, of each row; -1 for rows of no admitted request
+ *   free_left : one int32, what remains of the free list.  Apart from free_count, so that a call can be repeated
+ * Requests are admitted whole and in order: one whose new tokens fit neither the block table nor n_rows is passed over,
+ * and once the free list is too short for one that needs blocks, so it is for all after it that need any; lengths of those
+ * are what they held.  A table entry that is no block of the cache gives slot -1.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, ALIGN, HIP. */
+int nnv_kv_plan(const nnv_attention_desc *desc, int n_requests, int n_rows, const int32_t *held, const int32_t *fresh,
+                const int32_t *free_blocks, const int32_t *free_count, int32_t *block_table, int32_t *starts, int32_t *lengths,
+                int32_t *positions, int64_t *slots, int32_t *free_left, void *hip_stream);
+
+/* Norms and rotations of queries and keys, and keys and values into the cache, in one pass over a step's rows.
+ *   q, k, v : rows of heads x head_dim elements, ldq, ldk, ldv elements apart (parts of one projection's output as well as
+ *       tensors of their own).  q NULL: no queries; k and v NULL: no keys and values
+ *   q_weight, k_weight : head_dim float32; NULL: no norm of these.  h -> h / sqrt(mean(h^2) + eps) * weight, of each head
+ *   rope : positions x rotary_dim float32, of each position the cosines, then the sines of its rotary_dim / 2 angles
+ *       (NULL where rotary_dim is 0).  (a, b) -> (a cos - b sin, b cos + a sin)
+ *   positions, slots : n_rows int32 and int64, as nnv_kv_plan writes them
+ *   q_out, k_out : n_rows x heads x head_dim, without gaps, apart from q, k and v; k_out may be NULL where there is a cache
+ *   cache : keys as rotated and values go to slots[row]; NULL: nowhere
+ * Rows of a position below 0, or behind the rotation table, yield zeros and are not held; slots outside the cache
+ * are not written.  A slot may be given once.  Keys are computed in float64 up to their codes: a rounding in the last
+ * bit would move a code by a whole step.  A NaN is held as 0, an infinity as the largest magnitude.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, ALIGN, HIP. */
+int nnv_qk_norm_rope(const nnv_attention_desc *desc, int n_rows, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                     const float *q_weight, const float *k_weight, const float *rope, const int32_t *positions, const int64_t *slots, void *q_out,
+                     void *k_out, void *cache, void *hip_stream);
+
+/* The keys and values that n slots of the cache stand for (n x kv_heads x head_dim of desc.dtype each; either may be NULL).  Slots outside the
+ * cache give zeros.  Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, ALIGN, HIP. */
+int nnv_kv_read(const nnv_attention_desc *desc, int n, const int64_t *slots, const void *cache, void *k, void *v, void *hip_stream);
+
+/* Attention of a step's rows over the cache: for every row of request i at position p, softmax over the tokens j <= p of the
+ * request (j < lengths[i]; with a window: p - j < window or j < sinks) of scale * q . k[j], times v[j].  Scores, softmax and sums are
+ * float32; weights are rounded to desc.dtype for the matrix cores.
+ *   q, out : n_rows x q_heads x head_dim;  query head h reads key head h / (q_heads / kv_heads)
+ *   block_table, starts, lengths, positions : as nnv_kv_plan writes them (n_requests of them, n_rows positions)
+ *   workspace : >= nnv_kv_attention_workspace_bytes(desc, n_requests, n_rows) bytes, whatever its contents
+ * Rows that see nothing (position below 0, no request, length 0) yield zeros.  Tokens whose table entry is no block
+ * of the cache are not seen.  starts and lengths are clamped to what desc and n_rows allow.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
+size_t nnv_kv_attention_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows);
+int nnv_kv_attention(const nnv_attention_desc *desc, int n_requests, int n_rows, const void *q, const int32_t *block_table, const int32_t *starts,
+                     const int32_t *lengths, const int32_t *positions, const void *cache, void *out, void *workspace, size_t workspace_bytes,
+                     void *hip_stream);
 
 #ifdef __cplusplus
 }

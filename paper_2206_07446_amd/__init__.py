@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     nnv_transformed_bytes, nnv_workspace_bytes, nnv_transform_weights, nnv_transform_weights_grouped,
     nnv_conv_forward, nnv_conv_forward_relu, nnv_conv_forward_static, STATIC_SCRATCH_BYTES, nnv_conv_forward_grouped,
     nnv_conv_forward_grouped_workspace_bytes, FORWARD_RELU, nnv_time_layer, nnv_cold_stack, nnv_cache_write, nnv_cache_read, EXPORTS,
+    BF16, LinearDesc, AttentionDesc, nnv_linear_transformed_bytes, nnv_linear_workspace_bytes, nnv_linear_transform_weights, nnv_linear_forward,
+    nnv_kv_cache_bytes, nnv_kv_plan, nnv_qk_norm_rope, nnv_kv_read, nnv_kv_attention_workspace_bytes, nnv_kv_attention,
 )

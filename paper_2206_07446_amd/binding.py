@@ -8,7 +8,7 @@ import ctypes
 import importlib.util
 import os
 import warnings
-from ctypes import c_char_p, c_double, c_int, c_int32, c_size_t, c_void_p, POINTER, Structure, byref
+from ctypes import c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p, POINTER, Structure, byref
 
 from . import build as _build
 
@@ -19,13 +19,15 @@ MODULE_PATH = _build.MODULE
 DIRECT, IM2COL_GEMM, WINO_F2, WINO_F4, DEPTHWISE, WINO_F6 = range(6)
 KINDS = {"direct": DIRECT, "im2col_gemm": IM2COL_GEMM, "wino_f2": WINO_F2, "wino_f4": WINO_F4,
          "depthwise": DEPTHWISE, "wino_f6": WINO_F6}
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2      # BF16: the serving operators only
 
 EXPORTS = ("nnv_layout_version", "nnv_status_string", "nnv_last_hip_error", "nnv_kind_supported",
            "nnv_transformed_bytes", "nnv_workspace_bytes", "nnv_transform_weights",
            "nnv_transform_weights_grouped", "nnv_conv_forward", "nnv_conv_forward_relu", "nnv_conv_forward_static", "nnv_conv_forward_grouped",
            "nnv_conv_forward_grouped_workspace_bytes", "nnv_time_layer", "nnv_cold_stack", "nnv_cache_write",
-           "nnv_cache_read")
+           "nnv_cache_read", "nnv_linear_transformed_bytes", "nnv_linear_workspace_bytes", "nnv_linear_transform_weights",
+           "nnv_linear_forward", "nnv_kv_cache_bytes", "nnv_kv_plan", "nnv_qk_norm_rope", "nnv_kv_read",
+           "nnv_kv_attention_workspace_bytes", "nnv_kv_attention")
 
 
 class NnvError(RuntimeError):
@@ -51,6 +53,17 @@ class Timing(Structure):
 
 class CacheIo(Structure):
     _fields_ = [("total_ms", c_double), ("file_ms", c_double), ("bytes", c_double), ("direct_io", c_int32)]
+
+
+class LinearDesc(Structure):
+    """A product with weights held in 8 bits (nnv_linear_desc)."""
+    _fields_ = [(n, c_int32) for n in ("n", "k", "x_dtype", "y_dtype", "raw_dtype")]
+
+
+class AttentionDesc(Structure):
+    """An attention layer over a cache of blocks held in 4 bits (nnv_attention_desc)."""
+    _fields_ = [(n, c_int32) for n in ("q_heads", "kv_heads", "head_dim", "block_tokens", "blocks", "table_blocks", "rotary_dim", "rotary_interleaved",
+                                       "positions", "window", "sinks", "dtype")] + [("scale", c_float), ("eps", c_float)]
 
 
 _lib = None
@@ -104,6 +117,27 @@ def load():
     lib.nnv_cache_write.argtypes = [c_char_p, POINTER(ConvDesc), c_int, c_void_p, c_void_p]
     lib.nnv_cache_read.restype = c_int
     lib.nnv_cache_read.argtypes = [c_char_p, POINTER(ConvDesc), c_int, c_void_p, c_int, c_void_p, POINTER(CacheIo)]
+    lib.nnv_linear_transformed_bytes.restype = c_size_t
+    lib.nnv_linear_transformed_bytes.argtypes = [POINTER(LinearDesc)]
+    lib.nnv_linear_workspace_bytes.restype = c_size_t
+    lib.nnv_linear_workspace_bytes.argtypes = [POINTER(LinearDesc), c_int]
+    lib.nnv_linear_transform_weights.restype = c_int
+    lib.nnv_linear_transform_weights.argtypes = [POINTER(LinearDesc), c_void_p, c_void_p, c_void_p]
+    lib.nnv_linear_forward.restype = c_int
+    lib.nnv_linear_forward.argtypes = [POINTER(LinearDesc), c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_size_t,
+                                       c_void_p]
+    lib.nnv_kv_cache_bytes.restype = c_size_t
+    lib.nnv_kv_cache_bytes.argtypes = [POINTER(AttentionDesc)]
+    lib.nnv_kv_plan.restype = c_int
+    lib.nnv_kv_plan.argtypes = [POINTER(AttentionDesc), c_int, c_int] + [c_void_p] * 11
+    lib.nnv_qk_norm_rope.restype = c_int
+    lib.nnv_qk_norm_rope.argtypes = [POINTER(AttentionDesc), c_int] + [c_void_p, c_int64] * 3 + [c_void_p] * 9
+    lib.nnv_kv_read.restype = c_int
+    lib.nnv_kv_read.argtypes = [POINTER(AttentionDesc), c_int] + [c_void_p] * 5
+    lib.nnv_kv_attention_workspace_bytes.restype = c_size_t
+    lib.nnv_kv_attention_workspace_bytes.argtypes = [POINTER(AttentionDesc), c_int, c_int]
+    lib.nnv_kv_attention.restype = c_int
+    lib.nnv_kv_attention.argtypes = [POINTER(AttentionDesc), c_int, c_int] + [c_void_p] * 8 + [c_size_t, c_void_p]
     _native = _load_module(torch)
     _lib = lib
     return lib
@@ -122,6 +156,7 @@ def _load_module(torch):
         return _CtypesCalls
     native.setup(ConvDesc, _fail, lambda: torch.cuda.current_stream().cuda_stream, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
                  getattr(torch._C, "_cuda_getCurrentRawStream", None))
+    native.setup_serving(LinearDesc, AttentionDesc)
     return native
 
 
@@ -177,6 +212,13 @@ def _ptrs(tensors, n, null=False):
     return _array(c_void_p, tensors, n, lambda t: t if isinstance(t, int) or (null and t is None) else t.data_ptr())
 
 
+def _int(v):
+    """A count as the ABI takes it: ctypes would cut off what 32 bits do not hold."""
+    if not -(1 << 31) <= v < 1 << 31:
+        raise OverflowError("a count does not fit 32 bits")
+    return v
+
+
 def _size(workspace, count=None):
     if count is not None:
         return count
@@ -225,6 +267,36 @@ class _CtypesCalls:
         stx = se if stream_tx is None else _stream(stream_tx)
         _check(load().nnv_cold_stack(n, _array(ConvDesc, descs, n), _array(c_int, kinds, n), _ptrs(w_raw, n), _ptrs(w_tx, n), _ptrs(x, n),
                                      _ptrs(y, n), _ptr(workspace), _size(workspace), stage_layers, se, stx), "nnv_cold_stack")
+
+    @staticmethod
+    def linear_transform_weights(desc, w_raw, w_tx, stream):
+        _check(load().nnv_linear_transform_weights(byref(desc), _ptr(w_raw), _ptr(w_tx), _stream(stream)), "nnv_linear_transform_weights")
+
+    @staticmethod
+    def linear_forward(desc, m, x, ldx, w_tx, bias, y, ldy, workspace, workspace_bytes, stream):
+        _check(load().nnv_linear_forward(byref(desc), _int(m), _ptr(x), ldx, _ptr(w_tx), _ptr(bias), _ptr(y), ldy, _ptr(workspace),
+                                         _size(workspace, workspace_bytes), _stream(stream)), "nnv_linear_forward")
+
+    @staticmethod
+    def kv_plan(desc, n_requests, n_rows, *arrays_and_stream):
+        *arrays, stream = arrays_and_stream
+        _check(load().nnv_kv_plan(byref(desc), _int(n_requests), _int(n_rows), *[_ptr(t) for t in arrays], _stream(stream)), "nnv_kv_plan")
+
+    @staticmethod
+    def qk_norm_rope(desc, n_rows, q, ldq, k, ldk, v, ldv, *tensors_and_stream):
+        *tensors, stream = tensors_and_stream
+        _check(load().nnv_qk_norm_rope(byref(desc), _int(n_rows), _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, *[_ptr(t) for t in tensors],
+                                       _stream(stream)), "nnv_qk_norm_rope")
+
+    @staticmethod
+    def kv_read(desc, n, slots, cache, k, v, stream):
+        _check(load().nnv_kv_read(byref(desc), _int(n), _ptr(slots), _ptr(cache), _ptr(k), _ptr(v), _stream(stream)), "nnv_kv_read")
+
+    @staticmethod
+    def kv_attention(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes, stream):
+        _check(load().nnv_kv_attention(byref(desc), _int(n_requests), _int(n_rows), _ptr(q), _ptr(block_table), _ptr(starts), _ptr(lengths),
+                                       _ptr(positions), _ptr(cache), _ptr(out), _ptr(workspace), _size(workspace, workspace_bytes),
+                                       _stream(stream)), "nnv_kv_attention")
 
 
 def nnv_layout_version() -> int:
@@ -312,3 +384,50 @@ def nnv_cache_read(path: str, desc: ConvDesc, kind: int, w_tx, verify: bool = Fa
 def nnv_cold_stack(descs, kinds, w_raw, w_tx, x, y, workspace, stage_layers=1, stream_exec=None, stream_tx=None) -> None:
     """stream_tx=None runs both operations on stream_exec (the unpipelined order)."""
     (_native or _calls()).cold_stack(descs, kinds, w_raw, w_tx, x, y, workspace, stage_layers, stream_exec, stream_tx)
+
+
+# ---- operators of a language model's layer as a serving program runs it
+
+def nnv_linear_transformed_bytes(desc: LinearDesc) -> int:
+    return int(load().nnv_linear_transformed_bytes(byref(desc)))
+
+
+def nnv_linear_workspace_bytes(desc: LinearDesc, m: int) -> int:
+    return int(load().nnv_linear_workspace_bytes(byref(desc), _int(m)))
+
+
+def nnv_linear_transform_weights(desc: LinearDesc, w_raw, w_tx, stream=None) -> None:
+    (_native or _calls()).linear_transform_weights(desc, w_raw, w_tx, stream)
+
+
+def nnv_linear_forward(desc: LinearDesc, m: int, x, ldx: int, w_tx, bias, y, ldy: int, workspace, workspace_bytes=None, stream=None) -> None:
+    (_native or _calls()).linear_forward(desc, m, x, ldx, w_tx, bias, y, ldy, workspace, workspace_bytes, stream)
+
+
+def nnv_kv_cache_bytes(desc: AttentionDesc) -> int:
+    return int(load().nnv_kv_cache_bytes(byref(desc)))
+
+
+def nnv_kv_plan(desc: AttentionDesc, n_requests: int, n_rows: int, held, fresh, free_blocks, free_count, block_table, starts, lengths, positions,
+                slots, free_left, stream=None) -> None:
+    (_native or _calls()).kv_plan(desc, n_requests, n_rows, held, fresh, free_blocks, free_count, block_table, starts, lengths, positions, slots,
+                                  free_left, stream)
+
+
+def nnv_qk_norm_rope(desc: AttentionDesc, n_rows: int, q, ldq: int, k, ldk: int, v, ldv: int, q_weight, k_weight, rope, positions, slots, q_out, k_out,
+                     cache, stream=None) -> None:
+    (_native or _calls()).qk_norm_rope(desc, n_rows, q, ldq, k, ldk, v, ldv, q_weight, k_weight, rope, positions, slots, q_out, k_out, cache, stream)
+
+
+def nnv_kv_read(desc: AttentionDesc, n: int, slots, cache, k, v, stream=None) -> None:
+    (_native or _calls()).kv_read(desc, n, slots, cache, k, v, stream)
+
+
+def nnv_kv_attention_workspace_bytes(desc: AttentionDesc, n_requests: int, n_rows: int) -> int:
+    return int(load().nnv_kv_attention_workspace_bytes(byref(desc), _int(n_requests), _int(n_rows)))
+
+
+def nnv_kv_attention(desc: AttentionDesc, n_requests: int, n_rows: int, q, block_table, starts, lengths, positions, cache, out, workspace,
+                     workspace_bytes=None, stream=None) -> None:
+    (_native or _calls()).kv_attention(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes,
+                                       stream)

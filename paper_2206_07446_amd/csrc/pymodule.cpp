@@ -14,6 +14,7 @@
 
 namespace {
 
+PyObject *g_linear_type, *g_attention_type;                                     // handed over by setup_serving()
 PyObject *g_desc_type, *g_fail, *g_slow_stream, *g_get_device, *g_raw_stream;    // handed over by setup()
 PyObject *g_data_ptr, *g_numel, *g_element_size, *g_cuda_stream;                 // interned names
 bool g_stream_ready = false;     // torch has initialised the device: the raw calls may be used
@@ -31,15 +32,40 @@ bool as_pointer_or_null(PyObject *o, void **out) {
     return true;
 }
 
-bool as_desc(PyObject *o, nnv_conv_desc *out) {
-    if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject *>(g_desc_type))) {
-        PyErr_Format(PyExc_TypeError, "expected ConvDesc, got %.100s", Py_TYPE(o)->tp_name);
+template <typename T> bool as_struct(PyObject *o, PyObject *type, T *out) {
+    PyTypeObject *want = reinterpret_cast<PyTypeObject *>(type);
+    if (!want || !PyObject_TypeCheck(o, want)) {
+        PyErr_Format(PyExc_TypeError, "expected %.100s, got %.100s", want ? want->tp_name : "a descriptor", Py_TYPE(o)->tp_name);
         return false;
     }
     Py_buffer view;
     if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE)) return false;
-    memcpy(out, view.buf, sizeof(*out));
+    const bool fits = view.len == (Py_ssize_t)sizeof(*out);
+    if (fits) memcpy(out, view.buf, sizeof(*out));
+    else PyErr_Format(PyExc_TypeError, "%.100s of %zd bytes, %zd are wanted", Py_TYPE(o)->tp_name, view.len, (Py_ssize_t)sizeof(*out));
     PyBuffer_Release(&view);
+    return fits;
+}
+bool as_desc(PyObject *o, nnv_conv_desc *out) { return as_struct(o, g_desc_type, out); }
+
+bool as_int(PyObject *o, int *out) {
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) return false;
+    if (v != static_cast<int>(v)) {
+        PyErr_SetString(PyExc_OverflowError, "a count does not fit 32 bits");
+        return false;
+    }
+    *out = static_cast<int>(v);
+    return true;
+}
+bool as_int64(PyObject *o, int64_t *out) {
+    *out = PyLong_AsLongLong(o);
+    return !(*out == -1 && PyErr_Occurred());
+}
+template <typename T> bool as_address(PyObject *o, T **out) {
+    void *p;
+    if (!as_pointer_or_null(o, &p)) return false;
+    *out = static_cast<T *>(p);
     return true;
 }
 
@@ -246,6 +272,127 @@ PyObject *cold_stack(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return finish(rc, "nnv_cold_stack");
 }
 
+// ---- the serving operators: arguments in the order of nnv.h, the stream last
+
+// (desc, w_raw, w_tx, stream)
+PyObject *linear_transform_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_linear_desc d;
+    void *raw, *tx, *st;
+    if (!count_is(n, 4) || !as_struct(a[0], g_linear_type, &d) || !as_address(a[1], &raw) || !as_address(a[2], &tx) || !as_stream(a[3], &st)) return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_linear_transform_weights(&d, raw, tx, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_linear_transform_weights");
+}
+
+// (desc, m, x, ldx, w_tx, bias, y, ldy, workspace, workspace_bytes, stream)
+PyObject *linear_forward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_linear_desc d;
+    int m;
+    int64_t ldx, ldy;
+    void *x, *tx, *y, *ws, *st;
+    float *bias;
+    size_t bytes;
+    if (!count_is(n, 11) || !as_struct(a[0], g_linear_type, &d) || !as_int(a[1], &m) || !as_address(a[2], &x) || !as_int64(a[3], &ldx) ||
+        !as_address(a[4], &tx) || !as_address(a[5], &bias) || !as_address(a[6], &y) || !as_int64(a[7], &ldy) || !as_address(a[8], &ws) ||
+        !as_bytes(a[9], a[8], &bytes) || !as_stream(a[10], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_linear_forward(&d, m, x, ldx, tx, bias, y, ldy, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_linear_forward");
+}
+
+// (desc, n_requests, n_rows, held, fresh, free_blocks, free_count, block_table, starts, lengths, positions, slots, free_left, stream)
+PyObject *kv_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows;
+    int32_t *held, *fresh, *free_blocks, *count, *table, *starts, *lengths, *positions, *left;
+    int64_t *slots;
+    void *st;
+    if (!count_is(n, 14) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) || !as_address(a[3], &held) ||
+        !as_address(a[4], &fresh) || !as_address(a[5], &free_blocks) || !as_address(a[6], &count) || !as_address(a[7], &table) ||
+        !as_address(a[8], &starts) || !as_address(a[9], &lengths) || !as_address(a[10], &positions) || !as_address(a[11], &slots) ||
+        !as_address(a[12], &left) || !as_stream(a[13], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_plan(&d, requests, rows, held, fresh, free_blocks, count, table, starts, lengths, positions, slots, left, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_plan");
+}
+
+// (desc, n_rows, q, ldq, k, ldk, v, ldv, q_weight, k_weight, rope, positions, slots, q_out, k_out, cache, stream)
+PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int rows;
+    int64_t ldq, ldk, ldv, *slots;
+    void *q, *k, *v, *q_out, *k_out, *cache, *st;
+    float *qw, *kw, *rope;
+    int32_t *positions;
+    if (!count_is(n, 17) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &rows) || !as_address(a[2], &q) || !as_int64(a[3], &ldq) ||
+        !as_address(a[4], &k) || !as_int64(a[5], &ldk) || !as_address(a[6], &v) || !as_int64(a[7], &ldv) || !as_address(a[8], &qw) ||
+        !as_address(a[9], &kw) || !as_address(a[10], &rope) || !as_address(a[11], &positions) || !as_address(a[12], &slots) ||
+        !as_address(a[13], &q_out) || !as_address(a[14], &k_out) || !as_address(a[15], &cache) || !as_stream(a[16], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_qk_norm_rope(&d, rows, q, ldq, k, ldk, v, ldv, qw, kw, rope, positions, slots, q_out, k_out, cache, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_qk_norm_rope");
+}
+
+// (desc, n, slots, cache, k, v, stream)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int count;
+    int64_t *slots;
+    void *cache, *k, *v, *st;
+    if (!count_is(n, 7) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &count) || !as_address(a[2], &slots) || !as_address(a[3], &cache) ||
+        !as_address(a[4], &k) || !as_address(a[5], &v) || !as_stream(a[6], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_read(&d, count, slots, cache, k, v, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_read");
+}
+
+// (desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes, stream)
+PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows;
+    void *q, *cache, *out, *ws, *st;
+    int32_t *table, *starts, *lengths, *positions;
+    size_t bytes;
+    if (!count_is(n, 13) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) || !as_address(a[3], &q) ||
+        !as_address(a[4], &table) || !as_address(a[5], &starts) || !as_address(a[6], &lengths) || !as_address(a[7], &positions) ||
+        !as_address(a[8], &cache) || !as_address(a[9], &out) || !as_address(a[10], &ws) || !as_bytes(a[11], a[10], &bytes) || !as_stream(a[12], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_attention(&d, requests, rows, q, table, starts, lengths, positions, cache, out, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_attention");
+}
+
+// (LinearDesc type, AttentionDesc type)
+PyObject *setup_serving(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count_is(n, 2)) return nullptr;
+    PyObject **slots[2] = {&g_linear_type, &g_attention_type};
+    if (!PyType_Check(a[0]) || !PyType_Check(a[1])) {
+        PyErr_SetString(PyExc_TypeError, "the arguments are the descriptor types");
+        return nullptr;
+    }
+    for (int i = 0; i < 2; ++i) {
+        Py_INCREF(a[i]);
+        Py_XSETREF(*slots[i], a[i]);
+    }
+    Py_RETURN_NONE;
+}
+
 // (ConvDesc type, fail(status, where), current stream handle by torch's public call, current device, raw stream of a device or None)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!count_is(n, 5)) return nullptr;
@@ -264,7 +411,8 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define NNV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {NNV_METHOD(setup), NNV_METHOD(conv_forward), NNV_METHOD(conv_forward_relu), NNV_METHOD(conv_forward_static),
                            NNV_METHOD(conv_forward_grouped), NNV_METHOD(transform_weights), NNV_METHOD(transform_weights_grouped),
-                           NNV_METHOD(cold_stack), {nullptr, nullptr, 0, nullptr}};
+                           NNV_METHOD(cold_stack), NNV_METHOD(setup_serving), NNV_METHOD(linear_transform_weights), NNV_METHOD(linear_forward),
+                           NNV_METHOD(kv_plan), NNV_METHOD(qk_norm_rope), NNV_METHOD(kv_read), NNV_METHOD(kv_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nnvpy", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
