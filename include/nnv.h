@@ -307,11 +307,12 @@ typedef struct {
     int32_t raw_dtype;  /* nnv_dtype of the raw weights */
 } nnv_linear_desc;
 
-/* Bytes of the transformed weights (0 if the descriptor is invalid): one per weight of blocks of 128 x 128, and the scales. */
+/* Bytes of the transformed weights (0 if the descriptor is invalid): one per weight, rows filled up to
+ * a multiple of 128 and columns to one of 256, and the scales. */
 size_t nnv_linear_transformed_bytes(const nnv_linear_desc *desc);
 
-/* Bytes of scratch of nnv_linear_forward over m rows (0 if invalid): x in 8 bits with its scales, and where the
- * reduction of a few rows is split, partial sums. */
+/* Bytes of scratch of nnv_linear_forward over m rows (0 if invalid, or for up to 16 rows): x in 8 bits with its scales, and where
+ * the reduction is split, partial sums. */
 size_t nnv_linear_workspace_bytes(const nnv_linear_desc *desc, int m);
 
 /* Raw weights (n x k of desc.raw_dtype, rows of k) -> 8-bit codes in the order that the matrix instructions read, and scales.

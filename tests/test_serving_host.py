@@ -55,11 +55,12 @@ def test_scales_of_the_oracle():
 
 def test_linear_sizes(calls):
     assert nnv.nnv_linear_transformed_bytes(linear()) == 256 * 512 + 256
-    assert nnv.nnv_linear_transformed_bytes(linear(n=1, k=1)) == 128 * 128 + 256
-    assert nnv.nnv_linear_transformed_bytes(linear(n=129, k=513)) == 256 * 640 + 256
-    assert nnv.nnv_linear_workspace_bytes(linear(), 0) == 0 and nnv.nnv_linear_workspace_bytes(linear(), 1) > 0
-    for m in (1, 16, 17, 1000):
-        assert nnv.nnv_linear_workspace_bytes(linear(k=500), m) >= -(-m // 16) * 16 * 512
+    assert nnv.nnv_linear_transformed_bytes(linear(n=1, k=1)) == 128 * 256 + 256
+    assert nnv.nnv_linear_transformed_bytes(linear(n=129, k=513)) == 256 * 768 + 256
+    for m in (0, 1, 16):                                 # a few rows are rounded where they are used
+        assert nnv.nnv_linear_workspace_bytes(linear(), m) == 0
+    for m in (17, 32, 33, 1000):
+        assert nnv.nnv_linear_workspace_bytes(linear(k=500), m) >= (m > 16) * -(-m // 16) * 16 * 512
 
 
 @pytest.mark.parametrize("bad", [dict(n=0), dict(k=-1), dict(x_dtype=3), dict(y_dtype=-1), dict(raw_dtype=9), dict(n=1 << 23), dict(k=1 << 21)])
@@ -67,7 +68,7 @@ def test_linear_descriptors(calls, bad):
     d = linear(**bad)
     assert nnv.nnv_linear_transformed_bytes(d) == 0 and nnv.nnv_linear_workspace_bytes(d, 4) == 0
     assert status(nnv.nnv_linear_transform_weights, d, A, A) == BAD_DESC
-    assert status(nnv.nnv_linear_forward, d, 4, A, 512, A, None, A, 256, A, 1 << 30) == BAD_DESC
+    assert status(nnv.nnv_linear_forward, d, 40, A, 512, A, None, A, 256, A, 1 << 30) == BAD_DESC
 
 
 def test_linear_refusals(calls):
@@ -77,18 +78,18 @@ def test_linear_refusals(calls):
     f(d, 0, None, 0, None, None, None, 0, None, 0, stream=0)
     assert status(f, d, -1, A, 512, A, None, A, 256, A, big) == ARG
     assert status(f, d, 1 << 20, A, 512, A, None, A, 256, A, big) == ARG
-    assert status(f, d, 4, A, 511, A, None, A, 256, A, big) == ARG
-    assert status(f, d, 4, A, 512, A, None, A, 255, A, big) == ARG
+    assert status(f, d, 40, A, 511, A, None, A, 256, A, big) == ARG
+    assert status(f, d, 40, A, 512, A, None, A, 255, A, big) == ARG
     for i in (2, 4, 6):
-        args = [d, 4, A, 512, A, None, A, 256, A, big]
+        args = [d, 40, A, 512, A, None, A, 256, A, big]
         args[i] = None
         assert status(f, *args) == NULL
         args[i] = A + 4
         assert status(f, *args) == ALIGN
-    assert status(f, d, 4, A, 512, A, A + 2, A, 256, A, big) == ALIGN
-    assert status(f, d, 4, A, 512, A, None, A, 256, None, big) == NULL
-    assert status(f, d, 4, A, 512, A, None, A, 256, A, 16) == WORKSPACE
-    assert status(f, d, 4, A, 512, A, None, A, 256, torch.empty(8)) == WORKSPACE
+    assert status(f, d, 40, A, 512, A, A + 2, A, 256, A, big) == ALIGN
+    assert status(f, d, 40, A, 512, A, None, A, 256, None, big) == NULL
+    assert status(f, d, 40, A, 512, A, None, A, 256, A, 16) == WORKSPACE
+    assert status(f, d, 40, A, 512, A, None, A, 256, torch.empty(8)) == WORKSPACE
 
 
 @pytest.mark.parametrize("bad,want", [(dict(q_heads=0), BAD_DESC), (dict(q_heads=9), BAD_DESC), (dict(q_heads=2048), BAD_DESC), (dict(kv_heads=0), BAD_DESC),
