@@ -17,6 +17,7 @@ namespace nnv {
 constexpr int kStep = 32;          // tokens of a wavefront's step
 constexpr int kTileRows = 16;
 constexpr int kAttendWaves = 4;
+constexpr int kManyPairs = 32;     // pairs of a request from which on kv_attend_many takes it, where both kernels run
 
 template <int DT> struct Mfma;
 template <> struct Mfma<NNV_F16> {
@@ -54,55 +55,103 @@ __device__ static inline int row_max(int v) {
 }
 __device__ static inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// A tile of a request: which rows, and which steps of tokens they see: [0, sink_steps) and [first_step, first_step + steps - sink_steps).
+__device__ static inline int wave_max(int v) {
+    v = row_max(v);
+    v = max(v, __shfl_xor(v, 16));
+    return uniform(max(v, __shfl_xor(v, 32)));
+}
+
+// A tile of a request: R consecutive pairs of a row and a query head of the group.
 struct Tile {
-    int request, row0, pair0, pairs;     // first row of the request, first (row, head) pair of the tile, pairs in it
-    int position;                        // of the row of column lane % 16; -1 of a column that is no pair
-    int lowest, highest;                 // of the tile's positions; lowest -1 where a row sees nothing
-    int length, steps, sink_steps, first_step;
-    __device__ int step_at(int i) const { return i < sink_steps ? i : first_step + i - sink_steps; }
+    int request, row0, pair0, pairs;     // first row of the request, first pair of the tile, pairs in it
+    int request_pairs, length;
 };
 
-// Finds tile u.  Tiles of request i start at floor(starts[i] * group / 16) + i: enough for its pairs, with gaps; request `requests` stands for the
-// rows that belong to none.  Every wavefront does so by itself: 64 starts at a time are compared with u, so that 4096 requests
-// take two loads one after the other.  pairs = 0 for a gap.  Whatever starts, lengths and positions hold, the tile stays within a.rows rows.
-__device__ static inline Tile find_tile(const AttendArgs &a, int u) {
+// Whatever starts and lengths hold, a tile stays within a.rows rows.
+__device__ static inline int clamped_start(const AttendArgs &a, int v) { return min(max(v, 0), a.rows); }
+
+// Tile `local` of a request, from what starts and lengths hold for it.
+template <int R> __device__ static inline Tile tile_of(const AttendArgs &a, int request, int start, int end, int length, int64_t local) {
     Tile t;
+    const int64_t all = max((int64_t)(end - start) * a.group, (int64_t)0);
+    t.request = request;
+    t.row0 = start;
+    t.pair0 = (int)(local * R);
+    t.pairs = local < 0 ? 0 : (int)min(max(all - local * R, (int64_t)0), (int64_t)R);
+    t.request_pairs = (int)min(all, (int64_t)0x7fffffff);
+    t.length = (int)min((int64_t)max(length, 0), (int64_t)a.width << a.block_log);
+    return t;
+}
+
+// Finds tile u.  Tiles of request i start at floor(starts[i] * group / R) + i: enough for its pairs, with gaps (pairs = 0); request `requests`
+// stands for the rows that belong to none.  Every wavefront does so by itself: 64 starts at a time are compared with u, and in the last round,
+// the only one of up to 63 requests, come with the starts after them and the lengths, so that a chain of loads is one link long.
+template <int R> __device__ static inline Tile find_tile(const AttendArgs &a, int u) {
     const int lane = threadIdx.x & 63;
     int lo = 0, span = a.requests + 1;
-    while (span > 1) {
+    for (;;) {
         const int each = (span + 63) / 64, i = lo + lane * each;
-        const bool reached = lane * each < span && (int64_t)min(max(a.starts[i], 0), a.rows) * a.group / kTileRows + i <= u;
-        const int n = max(__builtin_popcountll(__ballot(reached)), 1);
-        lo += (n - 1) * each;
-        span = min(each, span - (n - 1) * each);
+        const bool mine = lane * each < span, request = mine && i < a.requests;
+        const int start = mine ? clamped_start(a, a.starts[i]) : a.rows;
+        const int end = each == 1 && request ? clamped_start(a, a.starts[i + 1]) : a.rows, length = each == 1 && request ? a.lengths[i] : 0;
+        const int n = max(__builtin_popcountll(__ballot(mine && (int64_t)start * a.group / R + i <= u)), 1);
+        lo = uniform(lo + (n - 1) * each);
+        span = uniform(min(each, span - (n - 1) * each));
+        if (each == 1) {
+            const int at = uniform(n - 1), from = __builtin_amdgcn_readlane(start, at);
+            return tile_of<R>(a, lo, from, __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(length, at), u - ((int64_t)from * a.group / R + lo));
+        }
     }
-    t.request = uniform(lo);
-    const int start = min(max(a.starts[t.request], 0), a.rows);
-    const int end = t.request < a.requests ? min(max(a.starts[t.request + 1], 0), a.rows) : a.rows;
-    const int local = u - ((int)((int64_t)start * a.group / kTileRows) + t.request);
-    const int64_t left = (int64_t)(end - start) * a.group - (int64_t)local * kTileRows;
-    t.row0 = start;
-    t.pair0 = local * kTileRows;
-    t.pairs = local < 0 ? 0 : (int)min(max(left, (int64_t)0), (int64_t)kTileRows);
-    t.length = t.request < a.requests ? (int)min((int64_t)max(a.lengths[t.request], 0), (int64_t)a.width << a.block_log) : 0;
-    const int col = lane % 16;
-    t.position = col < t.pairs ? a.positions[t.row0 + (t.pair0 + col) / a.group] : -1;
-    t.highest = uniform(row_max(t.position));
-    t.lowest = -uniform(row_max(col < t.pairs ? -max(t.position, -1) : -0x7fffffff));
-    // the lowest of the rows that see anything
-    const int seeing = t.lowest >= 0 ? t.lowest : -uniform(row_max(t.position >= 0 ? -t.position : -0x7fffffff));
-    const int end_token = min(t.highest, t.length - 1) + 1, end_step = (end_token + kStep - 1) / kStep;
-    t.sink_steps = a.window ? min((a.sinks + kStep - 1) / kStep, end_step) : 0;
-    t.first_step = max(a.window ? max(seeing - a.window + 1, 0) / kStep : 0, t.sink_steps);
-    t.steps = end_token > 0 ? t.sink_steps + max(0, end_step - t.first_step) : 0;
-    return t;
+}
+
+// Tile u of up to 63 requests with those of the longest requests first, and of each the last: every lane adds up the tiles of the
+// requests before its own.  The tiles that take longest then begin first, and the end of a launch is not theirs (4 prompts of 1024 rows over 1024 to
+// 6000 tokens: see kv_attend_many).
+template <int R> __device__ static inline Tile find_longest(const AttendArgs &a, int u) {
+    const int lane = threadIdx.x & 63;
+    const bool mine = lane <= a.requests, request = lane < a.requests;
+    const int start = mine ? clamped_start(a, a.starts[lane]) : a.rows, end = request ? clamped_start(a, a.starts[lane + 1]) : a.rows;
+    const int length = request ? a.lengths[lane] : mine ? 0 : -1;
+    const int tiles = (int)((max((int64_t)(end - start) * a.group, (int64_t)0) + R - 1) / R);
+    int before = 0;
+    for (int j = 0; j <= a.requests; ++j) {
+        const int other = __builtin_amdgcn_readlane(length, j);
+        if (other > length || (other == length && j < lane)) before += __builtin_amdgcn_readlane(tiles, j);
+    }
+    const uint64_t found = __ballot(mine && before <= u && u < before + tiles);
+    if (!found) {
+        Tile none{};
+        return none;
+    }
+    const int at = __builtin_ctzll(found);
+    return tile_of<R>(a, at, __builtin_amdgcn_readlane(start, at), __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(length, at),
+                      __builtin_amdgcn_readlane(before + tiles, at) - 1 - u);
+}
+
+// Which steps of S tokens rows at positions `lowest` (of those that see anything) to `highest` see: [0, sinks) and [first, first + count - sinks).
+struct Steps {
+    int count, sinks, first;
+    __device__ int at(int i) const { return i < sinks ? i : first + i - sinks; }
+};
+template <int S> __device__ static inline Steps steps_of(const AttendArgs &a, int lowest, int highest, int length) {
+    const int end_token = min(highest, length - 1) + 1, end = (end_token + S - 1) / S;
+    Steps s;
+    s.sinks = a.window ? min((a.sinks + S - 1) / S, end) : 0;
+    s.first = max(a.window ? max(lowest - a.window + 1, 0) / S : 0, s.sinks);
+    s.count = end_token > 0 ? s.sinks + max(0, end - s.first) : 0;
+    return s;
 }
 
 // Steps of a split: whole rounds of the wavefronts.
 __device__ static inline int steps_each(int steps, int splits) {
     const int rounds = (steps + kAttendWaves - 1) / kAttendWaves;
     return (rounds + splits - 1) / splits * kAttendWaves;
+}
+
+// Eight values of a query; their signs turned where the factor of the scores is negative, so that the kernels' own is not.
+__device__ static inline i32x4_t query_words(const void *p, int flip) {
+    const i32x4_t v = *static_cast<const i32x4_t *>(p);
+    return i32x4_t{v[0] ^ flip, v[1] ^ flip, v[2] ^ flip, v[3] ^ flip};
 }
 
 // What a wavefront loads of a step, as it lies in the cache.
@@ -126,9 +175,15 @@ template <int N> __device__ static inline void load_words(const char *p, uint32_
     }
 }
 
+// A request's row of the block table, in the address space of constants: nothing here writes it, and its entries are read by the scalar unit.
+typedef const __attribute__((address_space(4))) int32_t *TableRow;
+__device__ static inline TableRow table_row(const AttendArgs &a, int request) {
+    return reinterpret_cast<TableRow>(reinterpret_cast<uintptr_t>(a.table + (int64_t)request * a.width));
+}
+
 // Blocks of the two sixteens of a step (a sixteen lies in one block); -1: none, or behind the request's tokens.
 struct StepBlocks { int id[2]; };
-__device__ static inline StepBlocks blocks_of(const AttendArgs &a, const int32_t *table, int step, int length) {
+__device__ static inline StepBlocks blocks_of(const AttendArgs &a, TableRow table, int step, int length) {
     StepBlocks s;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -141,18 +196,19 @@ __device__ static inline StepBlocks blocks_of(const AttendArgs &a, const int32_t
 
 // Of a block that is none, block 0 is read in its place; its tokens are not seen.
 template <int DIM> __device__ static inline void load_step(const AttendArgs &a, int head, int step, StepBlocks blocks, Held<DIM> &h) {
-    const int lane = threadIdx.x & 63, col = lane % 16, g = lane / 16;
+    const uint32_t lane = threadIdx.x & 63, col = lane % 16, g = lane / 16;
     const KvLayout at{DIM, 1 << a.block_log};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int token = (step * kStep + i * 16) & (at.tokens - 1), id = max(blocks.id[i], 0);
         const char *p = a.cache + ((int64_t)id * a.kv_heads + head) * at.head_bytes();
-        load_words(p + token * (DIM / 2) + (col * (DIM / 2) + g * (DIM / 8)), h.key[i]);
-        load_words(p + (at.value_at() + token * (DIM / 2)) + (g * 16 + col) * (DIM / 8), h.value[i]);
-        const char *ks = p + (at.key_scale_at() + token * (DIM / 32)) + col * (DIM / 32);
-        if constexpr (DIM == 256) h.key_scale[i] = *reinterpret_cast<const uint16_t *>(ks + 2 * g);
-        else h.key_scale[i] = *reinterpret_cast<const uint8_t *>(ks + (DIM == 128 ? g : g / 2));
-        h.value_scale[i] = *reinterpret_cast<const uint32_t *>(p + (at.value_scale_at() + token * (DIM / 32)) + (g * (DIM / 32) + col * (DIM / 16) / 32) * 4);
+        const char *keys = p + token * (DIM / 2), *values = p + at.value_at() + token * (DIM / 2);
+        const char *key_scales = p + at.key_scale_at() + token * (DIM / 32), *value_scales = p + at.value_scale_at() + token * (DIM / 32);
+        load_words(keys + (col * (DIM / 2) + g * (DIM / 8)), h.key[i]);
+        if constexpr (DIM == 256) h.key_scale[i] = *reinterpret_cast<const uint16_t *>(key_scales + (col * (DIM / 32) + 2 * g));
+        else h.key_scale[i] = *reinterpret_cast<const uint8_t *>(key_scales + (col * (DIM / 32) + (DIM == 128 ? g : g / 2)));
+        load_words(values + (g * 16 + col) * (DIM / 8), h.value[i]);
+        h.value_scale[i] = *reinterpret_cast<const uint32_t *>(value_scales + (g * (DIM / 32) + col * (DIM / 16) / 32) * 4);
     }
 }
 
@@ -172,44 +228,53 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
     __shared__ float join_base[kAttendWaves][kTileRows], join_sum[kAttendWaves][kTileRows];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 16, g = lane / 16;
     const int u = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles, head = rest % a.kv_heads, split = rest / a.kv_heads;
-    const Tile t = find_tile(a, u);
-    if (t.pairs == 0) return;
-    const int each = steps_each(t.steps, a.splits), begin = split * each, end = min(t.steps, begin + each);
-    if (split > 0 && begin >= end) return;
-    const bool whole = each >= t.steps;                  // no other split has any steps
-
-    const int32_t *table = a.table + (int64_t)t.request * a.width;
-    Held<DIM> held;
-    StepBlocks blocks = {{-1, -1}}, next_blocks = {{-1, -1}};
-    if (begin + wave < end) {
-        blocks = blocks_of(a, table, t.step_at(begin + wave), t.length);
-        load_step<DIM>(a, head, t.step_at(begin + wave), blocks, held);
-        if (begin + wave + kAttendWaves < end) next_blocks = blocks_of(a, table, t.step_at(begin + wave + kAttendWaves), t.length);
-    }
-    const int pair = t.pair0 + col;
+    // beside kv_attend_many, requests of fewer than 32 pairs: two tiles each
+    static_assert(kManyPairs <= 2 * kTileRows, "two tiles hold them");
+    const Tile t = a.many ? tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2)
+                          : find_tile<kTileRows>(a, u);
+    if (t.pairs == 0 || (a.many && t.request_pairs >= kManyPairs)) return;
     const bool there = col < t.pairs;
-    const int row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group;
-    const int position = min(t.position, t.length - 1), last_sink = a.window ? t.position - a.window : -1;    // tokens up to this one are seen as sinks only
+    const int pair = t.pair0 + col, row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group, own = there ? a.positions[row] : -1;
     i32x4_t q[kQ];
 #pragma unroll
     for (int s = 0; s < kQ; ++s)
-        q[s] = there ? *reinterpret_cast<const i32x4_t *>(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + g * (DIM / 4) + s * 8)
-                     : i32x4_t{0, 0, 0, 0};
+        q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + g * (DIM / 4) + s * 8, a.flip) : i32x4_t{0, 0, 0, 0};
+    // Without a window the steps are those of the request's length, so that the first codes need not wait for the positions; the
+    // last of them may be masked whole.
+    Steps steps = {t.length > 0 ? (t.length + kStep - 1) / kStep : 0, 0, 0};
+    if (a.window) {
+        const int seeing = -uniform(row_max(own >= 0 ? -own : -0x7fffffff));
+        steps = steps_of<kStep>(a, seeing, uniform(row_max(own)), t.length);
+    }
+    const int each = steps_each(steps.count, a.splits), begin = split * each, end = min(steps.count, begin + each);
+    if (split > 0 && begin >= end) return;
+    const bool whole = each >= steps.count;              // no other split has any steps
+
+    const TableRow table = table_row(a, t.request);
+    // the last step of this wavefront is loaded again where there is no next one: a load that some rounds leave out would
+    // make every round wait for all that are on their way
+    Held<DIM> held_a, held_b;
+    StepBlocks blocks = {{-1, -1}}, next_blocks = {{-1, -1}};
+    const int first = begin + wave, last = first + (end - 1 - first) / kAttendWaves * kAttendWaves;
+    if (first < end) {
+        blocks = blocks_of(a, table, steps.at(first), t.length);
+        next_blocks = blocks_of(a, table, steps.at(min(first + kAttendWaves, last)), t.length);
+        load_step<DIM>(a, head, steps.at(first), blocks, held_a);
+    }
+    const int highest = uniform(row_max(own)), lowest = -uniform(row_max(there ? -max(own, -1) : -0x7fffffff));
+    const int position = min(own, t.length - 1), last_sink = a.window ? own - a.window : -1;    // tokens up to this one are seen as sinks only
     f32x4_t o[kJ];
 #pragma unroll
     for (int j = 0; j < kJ; ++j) o[j] = f32x4_t{0, 0, 0, 0};
     float base = -3.4028234663852886e38f, sum = 0;
-    const int full_to = min(t.lowest, t.length - 1);                       // steps that end here or before are seen by all rows,
-    const int full_from = a.window ? t.highest - a.window + 1 : 0;        // if they begin here or behind
+    const int full_to = min(lowest, t.length - 1);                       // steps that end here or before are seen by all rows,
+    const int full_from = a.window ? highest - a.window + 1 : 0;        // if they begin here or behind
 
-    for (int i = begin + wave; i < end; i += kAttendWaves) {
-        const int step = t.step_at(i);
-        Held<DIM> next;
-        StepBlocks later = {{-1, -1}};
-        if (i + kAttendWaves < end) {
-            load_step<DIM>(a, head, t.step_at(i + kAttendWaves), next_blocks, next);
-            if (i + 2 * kAttendWaves < end) later = blocks_of(a, table, t.step_at(i + 2 * kAttendWaves), t.length);
-        }
+    __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
+    auto round = [&](int i, Held<DIM> &held, Held<DIM> &next) {
+        const int step = steps.at(i);
+        load_step<DIM>(a, head, steps.at(min(i + kAttendWaves, last)), next_blocks, next);
+        const StepBlocks later = blocks_of(a, table, steps.at(min(i + 2 * kAttendWaves, last)), t.length);
         f32x4_t s[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -222,7 +287,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
         }
         float p[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4] * a.scale;
+        for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4];
         const int token0 = step * kStep;
         if (token0 + kStep - 1 > full_to || (token0 < full_from && token0 + kStep > a.sinks) || blocks.id[0] < 0 || blocks.id[1] < 0) {
 #pragma unroll
@@ -240,7 +305,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
                     held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
                 }
         }
-        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+        float top = a.scale * fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
         if (__any(top > base + 8.f)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -251,7 +316,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             for (int j = 0; j < kJ; ++j) o[j] *= keep;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(p[e] - base);
+        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale, -base));
         sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         const i32x4_t weights = {round_pair<DT>(p[0], p[1]), round_pair<DT>(p[2], p[3]), round_pair<DT>(p[4], p[5]), round_pair<DT>(p[6], p[7])};
         // values: words of eight codes, kJ codes to a token
@@ -281,9 +346,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             o[2 * jj] = Mfma<DT>::dot(even, weights, o[2 * jj]);
             o[2 * jj + 1] = Mfma<DT>::dot(odd, weights, o[2 * jj + 1]);
         }
-        held = next;
         blocks = next_blocks;
         next_blocks = later;
+    };
+    // two rounds at a time, so that codes stay in the registers that they were loaded into
+    for (int i = first; i < end;) {
+        round(i, held_a, held_b);
+        i += kAttendWaves;
+        if (i >= end) break;
+        round(i, held_b, held_a);
+        i += kAttendWaves;
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -318,9 +390,258 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             if (half == 0 && d == 0 && a.splits > 1) {
                 part[DIM] = m;
                 part[DIM + 1] = l;
-                part[DIM + 2] = __builtin_bit_cast(float, whole ? 1 : (t.steps + each - 1) / each);
+                part[DIM + 2] = __builtin_bit_cast(float, whole ? 1 : (steps.count + each - 1) / each);
             }
         }
+    }
+}
+
+// Requests of many rows: a workgroup holds 128 pairs, 32 to a wavefront, and goes over the tokens 64 at a time.  Each wavefront turns the codes of 16
+// of them into operands in the LDS, once for all 128 pairs, where kv_attend would do so for every 16; the codes of the tokens after
+// that are on their way meanwhile.  Keys lie there as [32 tokens][16 values][8 of them][token], values as [32 values][16 tokens][8 of them][value],
+// every 16 bytes a lane's part of an operand.  The four lanes' worth of a token's values that a lane has in hand go to rows that lie 8 apart;
+// the row is xor-ed with its sixteen, so that they meet different banks, and reading does so as well.
+constexpr int kManyStep = 64, kManyRows = 128;
+
+template <int DT> struct Mfma32;
+template <> struct Mfma32<NNV_F16> {
+    static __device__ f32x16_t dot(i32x4_t a, i32x4_t b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Mfma<NNV_F16>::V8, a), __builtin_bit_cast(Mfma<NNV_F16>::V8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma32<NNV_BF16> {
+    static __device__ f32x16_t dot(i32x4_t a, i32x4_t b, f32x16_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Mfma<NNV_BF16>::V8, a), __builtin_bit_cast(Mfma<NNV_BF16>::V8, b), c, 0, 0, 0);
+    }
+};
+
+// What a wavefront loads of its 16 tokens: of a lane's token and quarter of a head the key's codes, of two fours of tokens the values'.
+template <int DIM> struct HeldMany { uint32_t key[DIM / 32], key_scale, value[2][DIM / 32], value_scale[2]; };
+
+template <int DIM> __device__ static inline void load_many(const AttendArgs &a, int head, int token0, int id, HeldMany<DIM> &h) {
+    const int lane = threadIdx.x & 63, col = lane % 16, g = lane / 16;
+    const KvLayout at{DIM, 1 << a.block_log};
+    const int token = token0 & (at.tokens - 1);
+    const char *p = a.cache + ((int64_t)max(id, 0) * a.kv_heads + head) * at.head_bytes();
+    load_words(p + token * (DIM / 2) + (col * (DIM / 2) + g * (DIM / 8)), h.key);
+    const char *ks = p + (at.key_scale_at() + token * (DIM / 32)) + col * (DIM / 32);
+    if constexpr (DIM == 256) h.key_scale = *reinterpret_cast<const uint16_t *>(ks + 2 * g);
+    else h.key_scale = *reinterpret_cast<const uint8_t *>(ks + (DIM == 128 ? g : g / 2));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int four = g % 2 + 2 * k;
+        load_words(p + (at.value_at() + token * (DIM / 2)) + (four * 16 + col) * (DIM / 8), h.value[k]);
+        h.value_scale[k] = *reinterpret_cast<const uint32_t *>(p + (at.value_scale_at() + token * (DIM / 32)) + (four * (DIM / 32) + col * (DIM / 16) / 32) * 4);
+    }
+}
+
+template <int DT, int DIM>
+__global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(AttendArgs a) {
+    typedef typename Elem<DT>::type T;
+    constexpr int kQ = DIM / 16, kJ = DIM / 16, kD = DIM / 32;
+    __shared__ i32x4_t keys[2][2][kQ][2][32], values[2][kD][4][2][32];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 32, half = lane / 32;
+    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % a.many_tiles, split = rest / a.many_tiles;
+    const Tile t = a.requests < 64 ? find_longest<kManyRows>(a, u) : find_tile<kManyRows>(a, u);
+    if (t.pairs == 0 || (t.request < a.requests && t.request_pairs < kManyPairs)) return;
+    // positions: of the tile for the steps, of the wavefront for its masks
+    auto position_of = [&](int i) { return i < t.pairs ? a.positions[t.row0 + (t.pair0 + i) / a.group] : -1; };
+    const int p0 = position_of(lane), p1 = position_of(lane + 64);
+    const int highest = wave_max(max(p0, p1));
+    const int seeing = -wave_max(max(p0 >= 0 ? -p0 : -0x7fffffff, p1 >= 0 ? -p1 : -0x7fffffff));
+    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length);
+    const int each = (steps.count + a.splits - 1) / a.splits, begin = split * each, end = min(steps.count, begin + each);
+    if (split > 0 && begin >= end) return;
+    const bool whole = each >= steps.count;
+
+    const TableRow table = table_row(a, t.request);
+    auto block_of = [&](int step) {                       // of the wavefront's sixteen tokens
+        const int token0 = step * kManyStep + wave * 16;
+        const int id = token0 < t.length ? table[token0 >> a.block_log] : -1;
+        return id >= 0 && id < a.blocks ? id : -1;
+    };
+    HeldMany<DIM> held;
+    int id = -1, next_id = -1;
+    auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
+    if (begin < end) {
+        id = block_of(steps.at(begin));
+        load_many<DIM>(a, head, steps.at(begin) * kManyStep + wave * 16, id, held);
+        next_id = block_of(clamped(begin + 1));
+    }
+    const int i0 = wave * 32 + col, pair = t.pair0 + i0;
+    const bool there = i0 < t.pairs, idle = wave * 32 >= t.pairs;
+    const int own = position_of(i0);
+    const int row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group;
+    const int position = min(own, t.length - 1), last_sink = a.window ? own - a.window : -1;
+    const int wave_lowest = -wave_max(there ? -max(own, -1) : -0x7fffffff), wave_highest = wave_max(own);
+    const int full_to = min(wave_lowest, t.length - 1), full_from = a.window ? wave_highest - a.window + 1 : 0;
+    i32x4_t q[kQ];
+#pragma unroll
+    for (int s = 0; s < kQ; ++s)
+        q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + s * 16 + half * 8, a.flip) : i32x4_t{0, 0, 0, 0};
+    f32x16_t o[kD];
+#pragma unroll
+    for (int d = 0; d < kD; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0;
+    float base = -3.4028234663852886e38f, sum = 0;
+
+    // the wavefront's sixteen tokens of a step into a buffer
+    auto spread = [&](int step, int buffer) {
+        const int c = lane % 16, g = lane / 16, h = g % 2, upper = g / 2, token0 = step * kManyStep + wave * 16;
+#pragma unroll
+        for (int i = 0; i < DIM / 32; ++i) {
+            const uint32_t byte = DIM != 256 ? held.key_scale : i >= DIM / 64 ? held.key_scale >> 8 : held.key_scale & 255;
+            const int octet_at = g * (DIM / 32) + i;
+            keys[buffer][wave / 2][octet_at / 2][octet_at % 2][wave % 2 * 16 + c] = octet<DT>(held.key[i], scale_of_byte(byte));
+        }
+        if (id < 0 || token0 + 16 > t.length) {            // what is not held may be anything: its values are to be finite, its scores are masked
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool is = id >= 0 && token0 + (h + 2 * k) * 4 + r < t.length;
+                    held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
+                }
+        }
+        uint32_t words[2][4];
+        float scale[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                scale[k][r] = scale_of_byte((held.value_scale[k] >> (8 * r)) & 255);
+                if constexpr (DIM == 256) words[k][r] = upper ? held.value[k][2 * r + 1] : held.value[k][2 * r];
+                else if constexpr (DIM == 128) words[k][r] = held.value[k][r] >> (16 * upper);
+                else words[k][r] = held.value[k][r / 2] >> (16 * (r % 2) + 8 * upper);
+            }
+        auto pair_at = [&](int k, int r, int jj) {
+            const uint32_t w = words[k][r];
+            return (uint32_t)(jj == 0 ? Mfma<DT>::template pair<0>(w, scale[k][r]) : jj == 1 ? Mfma<DT>::template pair<1>(w, scale[k][r])
+                            : jj == 2 ? Mfma<DT>::template pair<2>(w, scale[k][r]) : Mfma<DT>::template pair<3>(w, scale[k][r]));
+        };
+#pragma unroll
+        for (int jj = 0; jj < kJ / 4; ++jj) {
+            i32x4_t even, odd;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const uint32_t x = pair_at(k, r, jj), y = pair_at(k, r + 1, jj);
+                    even[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x05040100);
+                    odd[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x07060302);
+                }
+            const int d = c * kJ + upper * (kJ / 2) + 2 * jj;
+            values[buffer][d / 32][wave][h][(d % 32) ^ (d / 16)] = even;
+            values[buffer][d / 32][wave][h][((d + 1) % 32) ^ (d / 16)] = odd;
+        }
+    };
+    // a bit for each sixteen of a step that is a block of the cache: scalar, the same for all wavefronts
+    auto present = [&](int step) {
+        int bits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int token0 = step * kManyStep + i * 16;
+            const int b = token0 < t.length ? table[token0 >> a.block_log] : -1;
+            bits |= (b >= 0 && b < a.blocks ? 1 : 0) << i;
+        }
+        return bits;
+    };
+    int here = 0, here_next = 0;
+    if (begin < end) {
+        here = present(steps.at(begin));
+        here_next = present(clamped(begin + 1));
+        spread(steps.at(begin), 0);
+        id = next_id;
+        load_many<DIM>(a, head, clamped(begin + 1) * kManyStep + wave * 16, id, held);
+        next_id = block_of(clamped(begin + 2));
+    }
+    __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
+    __syncthreads();
+    for (int i = begin; i < end; ++i) {
+        const int step = steps.at(i), buffer = (i - begin) & 1, token0 = step * kManyStep;
+        const int here_later = present(clamped(i + 2));
+        if (!idle && token0 <= min(wave_highest, t.length - 1)) {
+            f32x16_t s[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = 0;
+#pragma unroll
+            for (int d = 0; d < kQ; ++d)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) s[b] = Mfma32<DT>::dot(keys[buffer][b][d][half][col], q[d], s[b]);
+            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || here != 15) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int token = token0 + b * 32 + 8 * (r / 4) + 4 * half + r % 4;
+                        const bool seen = (here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks);
+                        s[b][r] = seen ? s[b][r] : -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            top *= a.scale;
+            if (__any(top > base + 8.f)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(base, top), keep = __builtin_amdgcn_exp2f(base - now);
+                base = now;
+                sum *= keep;
+#pragma unroll
+                for (int d = 0; d < kD; ++d) o[d] *= keep;
+            }
+            float part[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale, -base));
+                part[e % 4] += s[e / 16][e % 16];
+            }
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const f32x16_t &p = s[k / 2];
+                const int r = k % 2 * 8;
+                const i32x4_t weights = {round_pair<DT>(p[r], p[r + 1]), round_pair<DT>(p[r + 2], p[r + 3]), round_pair<DT>(p[r + 4], p[r + 5]),
+                                         round_pair<DT>(p[r + 6], p[r + 7])};
+#pragma unroll
+                for (int d = 0; d < kD; ++d) o[d] = Mfma32<DT>::dot(values[buffer][d][k][half][col ^ (2 * d + col / 16)], weights, o[d]);
+            }
+        }
+        spread(clamped(i + 1), buffer ^ 1);
+        id = next_id;
+        load_many<DIM>(a, head, clamped(i + 2) * kManyStep + wave * 16, id, held);
+        next_id = block_of(clamped(i + 3));
+        here = here_next;
+        here_next = here_later;
+        __syncthreads();
+    }
+    sum += __shfl_xor(sum, 32);
+    if (!there) return;
+    // lane: pair col, values 32 d + 8 (r / 4) + 4 half + r % 4
+    const int64_t out_row = (int64_t)row * a.q_heads + qh;
+    float *parts = a.parts + (out_row * a.splits + split) * (DIM + kPartExtra);
+    const float inverse = sum > 0 ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int d = 0; d < kD; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int at = 32 * d + 2 * r + 4 * half;
+            if (whole) {
+                ElemVec<DT, 4> y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = (T)(o[d][r + j] * inverse);
+                *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + out_row * DIM + at) = y;
+            } else {
+                *reinterpret_cast<f32x4_t *>(parts + at) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+            }
+        }
+    if (a.splits > 1 && half == 0) {
+        parts[DIM] = base;
+        parts[DIM + 1] = sum;
+        parts[DIM + 2] = __builtin_bit_cast(float, whole ? 1 : (steps.count + each - 1) / each);
     }
 }
 
@@ -336,17 +657,20 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     __shared__ f32x4_t part[kGroups][kLanes];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float *p = a.parts + (int64_t)blockIdx.x * a.splits * (DIM + kPartExtra);
+    // (what is read of splits that there are not is not used)
+    const bool slot = tid < a.splits;
+    const float own_base = slot ? p[tid * (DIM + kPartExtra) + DIM] : 0.f, own_sum = slot ? p[tid * (DIM + kPartExtra) + DIM + 1] : 0.f;
     const int splits = __builtin_bit_cast(int, p[DIM + 2]);
     if (splits <= 1) return;
     const bool mine = tid < splits;
-    const float base = mine ? p[tid * (DIM + kPartExtra) + DIM] : -3.4028234663852886e38f;
+    const float base = mine ? own_base : -3.4028234663852886e38f;
     float m = base;
     for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
     if (lane == 0) bases[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(bases[0], bases[1]), fmaxf(bases[2], bases[3]));
     const float f = mine ? __builtin_amdgcn_exp2f(base - m) : 0.f;
-    float l = mine ? p[tid * (DIM + kPartExtra) + DIM + 1] * f : 0.f;
+    float l = mine ? own_sum * f : 0.f;
     for (int s = 1; s < 64; s *= 2) l += __shfl_xor(l, s);
     if (lane == 0) sums[wave] = l;
     if (mine) factor[tid] = f;
@@ -367,11 +691,15 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + (int64_t)blockIdx.x * DIM + 4 * at) = y;
 }
 
-static int attend_tiles(int requests, int rows, int group) { return (int)(((int64_t)rows * group) / kTileRows) + requests + 1; }
+static int attend_tiles(int requests, int rows, int group, int tile) { return (int)(((int64_t)rows * group) / tile) + requests + 1; }
 
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows) {
     return ((int64_t)rows * (d.q_heads / d.kv_heads) / kTileRows + requests + 1) * d.kv_heads;
 }
+
+// Whether a request of many rows is to be expected: then both kernels run, each on the requests it is for.  (16 requests of 4 rows, group 4:
+// 18 us by kv_attend, 21 with a launch beside it that finds nothing; 4 requests of 1024 rows: 387 us by kv_attend, 323 by both.)
+static bool attend_many(const nnv_attention_desc &d, int requests, int rows) { return (int64_t)(rows - requests) * (d.q_heads / d.kv_heads) >= 512; }
 
 // Splits of a tile's tokens, from what the host knows: 1024 workgroups where there are that few (four to a compute unit; with 512 to 4096 one
 // request of 32768 tokens and 8 heads takes the same 20 us), of at least 512 tokens (with 256 it takes 24 us, more partial
@@ -379,11 +707,12 @@ int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows)
 static int attend_splits(const nnv_attention_desc &d, int requests, int rows) {
     const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens;
     const int64_t reach = d.window && (int64_t)d.window + d.sinks < capacity ? (int64_t)d.window + d.sinks : capacity;
+    const bool many = attend_many(d, requests, rows);
     const int64_t pairs = (int64_t)rows * (d.q_heads / d.kv_heads), least = requests < rows ? requests : rows;
-    const int64_t tiles = pairs / kTileRows > least ? pairs / kTileRows : least;
-    const int64_t groups = (tiles > 0 ? tiles : 1) * d.kv_heads;
-    int64_t s = (1024 + groups - 1) / groups;
-    const int64_t longest = groups >= 2048 ? 8192 : 2048;
+    const int64_t full = pairs / (many ? kManyRows : kTileRows), tiles = full > least ? full : least;
+    const int64_t groups = (tiles > 0 ? tiles : 1) * d.kv_heads, fill = many ? 512 : 1024;
+    int64_t s = (fill + groups - 1) / groups;
+    const int64_t longest = groups >= 2 * fill || many ? 8192 : 2048;
     if (s < (reach + longest - 1) / longest) s = (reach + longest - 1) / longest;
     if (s > (reach + 511) / 512) s = (reach + 511) / 512;
     if (s > kMostSplits) s = kMostSplits;
@@ -398,8 +727,13 @@ size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, i
 }
 
 template <int DT, int DIM> static hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t st) {
-    kv_attend<DT, DIM><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
-    hipError_t e = hipGetLastError();
+    if (a.many) {
+        kv_attend_many<DT, DIM><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.tiles) kv_attend<DT, DIM><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
     return hipGetLastError();
@@ -410,7 +744,9 @@ template <int DT> static hipError_t launch_attend_type(const AttendArgs &a, int 
 
 hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
     AttendArgs a = args;
-    a.tiles = attend_tiles(a.requests, a.rows, a.group);
+    a.many = attend_many(d, a.requests, a.rows);
+    a.tiles = a.many ? 2 * a.requests : attend_tiles(a.requests, a.rows, a.group, kTileRows);
+    a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
     a.splits = attend_splits(d, a.requests, a.rows);
     a.parts = static_cast<float *>(ws);
     return d.dtype == NNV_F16 ? launch_attend_type<NNV_F16>(a, d.head_dim, st) : launch_attend_type<NNV_BF16>(a, d.head_dim, st);

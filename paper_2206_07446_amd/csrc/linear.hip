@@ -286,11 +286,12 @@ __global__ __launch_bounds__(64 * kRowWaves) void linear_rows(LinearArgs a, cons
         const int at = kb * 128 + quarter * 32;
         load32<DX, VEC>(x, row * ldx + at, row < a.m ? k - at : 0, v);
     };
+    const int last = a.kblocks - 1;                      // behind it, it is loaded again (see linear_waves)
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) {
-        const int kb = wave + kRowWaves * d;
-        if (kb < a.kblocks) fetch_weights(kb, ring[d]);
-        if (d < 2 && kb < a.kblocks) fetch_inputs(kb, inputs[d]);
+        const int kb = min(wave + kRowWaves * d, last);
+        fetch_weights(kb, ring[d]);
+        if (d < 2) fetch_inputs(kb, inputs[d]);
     }
     for (int base = wave; base < a.kblocks; base += kRowWaves * kAhead) {
 #pragma unroll
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void linear_rows(LinearArgs a, cons
             const int kb = base + kRowWaves * d, later = kb + kRowWaves * kAhead;
             if (kb < a.kblocks) {
                 const Inputs32<DX> v = inputs[d % 2];
-                if (kb + 2 * kRowWaves < a.kblocks) fetch_inputs(kb + 2 * kRowWaves, inputs[d % 2]);
+                fetch_inputs(min(kb + 2 * kRowWaves, last), inputs[d % 2]);
                 uint32_t amax = amax_bits32(v);
                 amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
                 amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void linear_rows(LinearArgs a, cons
                         acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(ring[d][t][2 * s], ring[d][t][2 * s + 1], sw), xv, acc[t], 0, 0, 0);
                 }
             }
-            if (later < a.kblocks) fetch_weights(later, ring[d]);
+            fetch_weights(min(later, last), ring[d]);
         }
     }
     __shared__ f32x4_t part[kRowWaves][NT][64];
@@ -557,10 +558,12 @@ __global__ __launch_bounds__(256, 2) void linear_waves(LinearArgs a) {
         for (int j = 0; j < FM; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    // a step behind the last is loaded as the last again: a load that some rounds leave out would make every round wait for all on their way
     Operands ring[kAhead];
+    const int last = step1 - 1;
+    if (step0 < step1)
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d)
-        if (step0 + wave + 4 * d < step1) fetch(step0 + wave + 4 * d, ring[d]);
+        for (int d = 0; d < kAhead; ++d) fetch(min(step0 + wave + 4 * d, last), ring[d]);
     for (int base = step0 + wave; base < step1; base += 4 * kAhead) {
 #pragma unroll
         for (int d = 0; d < kAhead; ++d) {
@@ -569,7 +572,7 @@ __global__ __launch_bounds__(256, 2) void linear_waves(LinearArgs a) {
                 const int byte = step / 2 % 4;
                 multiply<EXACT, FN, FM>(ring[d].w, ring[d].x, ring[d].sw >> (8 * byte), [&](int j) { return ring[d].sx[j] >> (8 * byte); }, acc);
             }
-            if (step + 4 * kAhead < step1) fetch(step + 4 * kAhead, ring[d]);
+            fetch(min(step + 4 * kAhead, last), ring[d]);
         }
     }
     // all sums into the LDS, a quarter of each out of it by every wavefront

@@ -57,8 +57,9 @@ struct AttendArgs {
     void *out;
     float *parts;
     int requests, rows, q_heads, kv_heads, group, block_log, blocks, width, window, sinks;
-    int tiles, splits;
-    float scale;        // of the scores, times log2(e)
+    int tiles, splits, many, many_tiles;       // many: requests of many rows go to a kernel of their own
+    float scale;        // magnitude of the factor of the scores, times log2(e); never 0, so that a score of -infinity stays one
+    int flip;           // sign bits of a pair of 16-bit values where the factor is negative
 };
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows);     // tiles of rows times key/value heads
 size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, int rows);

@@ -57,6 +57,25 @@ def test_sizes(m, n, k):
     check(y, *OS.linear(x.double().numpy(), w.double().numpy()), k, nnv.F32)
 
 
+# one of each way a product is run: few rows with 32 and 64 outputs to a workgroup, a reduction split among workgroups (evenly and not),
+# tiles of 128 in one part and several, tiles of 256
+WAYS = [(2, 6201, 260), (16, 12301, 130), (40, 300, 4300), (33, 250, 8300), (130, 6200, 2300), (260, 5001, 1030), (140, 20500, 140), (2500, 4900, 200), (4200, 3000, 384)]
+
+
+@pytest.mark.parametrize("m,n,k", WAYS)
+@pytest.mark.parametrize("y_dtype", [nnv.F32, nnv.BF16])
+def test_ways(m, n, k, y_dtype):
+    y, x, w, b = run(m, n, k, nnv.BF16, y_dtype, nnv.BF16, True, seed=11)
+    ref, size = OS.linear(x.double().numpy(), w.double().numpy(), b.double().numpy())
+    size += np.abs(b.double().numpy())
+    if y_dtype == nnv.F32:
+        return check(y, ref, size, k, y_dtype)
+    # 8-bit instructions line the products of eight inputs up to the largest and drop what is 2^17 below it: at most 2^-16 of the sum of magnitudes
+    got = y.double().cpu().numpy()
+    bound = ((k + 2) * 2.0 ** -23 + 2.0 ** -16) * size + 2.0 ** -8 * np.abs(ref) * (1 + 2.0 ** -8)
+    assert np.isfinite(got).all() and (np.abs(got - ref) <= bound).all(), (np.abs(got - ref) / bound).max()
+
+
 @pytest.mark.parametrize("x_dtype", [nnv.F32, nnv.F16, nnv.BF16])
 @pytest.mark.parametrize("y_dtype", [nnv.F32, nnv.F16, nnv.BF16])
 @pytest.mark.parametrize("m", [5, 150])
