@@ -336,7 +336,7 @@ typedef struct {
     int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads, at most 1024 */
     int32_t head_dim;           /* 64, 128 or 256 */
     int32_t block_tokens;       /* tokens of a cache block: 16, 32, 64, 128 or 256 */
-    int32_t blocks;             /* blocks of the cache */
+    int32_t blocks;             /* blocks of the cache, at most 2^30 */
     int32_t table_blocks;       /* columns of the block table: the most blocks of one request */
     int32_t rotary_dim;         /* leading values of a head that are rotated: even, 0 to head_dim */
     int32_t rotary_interleaved; /* 1: neighbours (2i, 2i + 1) turn together; 0: i and i + rotary_dim / 2 */

@@ -9,109 +9,138 @@ namespace nnv {
 
 constexpr int kPlanThreads = 256, kPlanEach = 4, kPlanChunk = kPlanThreads * kPlanEach;
 
-// Exclusive sum over the workgroup's threads; total is everybody's.
-__device__ static inline int64_t block_scan(int64_t v, int64_t *scratch, int64_t &total) {
+// Counts are added up to kMany and no further: more than any launch has rows or any cache blocks, so that nothing wraps around.
+constexpr int kMany = 1 << 30;
+__device__ static inline int add_up(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)kMany); }
+
+// Exclusive sum over the workgroup's threads of counts of 0 to kMany; total is everybody's.  Lanes of a wavefront by shifts within rows of 16 and broadcasts
+// between those, wavefronts through the LDS (scratch, by turns one of two).
+__device__ static inline int block_scan(int v, int *scratch, int &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t incl = v;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-        const int64_t o = __shfl_up(incl, s);
-        if (lane >= s) incl += o;
-    }
-    __syncthreads();                       // the scratch of the scan before has been read
+    int incl = v;
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x111, 0xf, 0xf, false));
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x112, 0xf, 0xf, false));
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x114, 0xf, 0xf, false));
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x118, 0xf, 0xf, false));
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x142, 0xa, 0xf, false));
+    incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x143, 0xc, 0xf, false));
     if (lane == 63) scratch[wave] = incl;
     __syncthreads();
-    int64_t before = 0;
+    int before = __shfl_up(incl, 1);
+    if (lane == 0) before = 0;
     total = 0;
 #pragma unroll
     for (int i = 0; i < kPlanThreads / 64; ++i) {
-        if (i < wave) before += scratch[i];
-        total += scratch[i];
+        if (i < wave) before = add_up(before, scratch[i]);
+        total = add_up(total, scratch[i]);
     }
-    return before + incl - v;
+    return before;
+}
+
+// The last of a chunk's requests whose `from` is at `at` or before it.
+__device__ static inline int last_from(const int *from, int last, int at) {
+    int i = 0;
+#pragma unroll
+    for (int step = kPlanChunk / 2; step; step /= 2)
+        if (i + step <= last && from[i + step] <= at) i += step;
+    return i;
 }
 
 // Every workgroup sums over all requests, 1024 at a time (two prefix sums: rows, then blocks needed), and writes the rows of its
-// own range; the requests' own outputs and table entries are written by the workgroup whose turn the chunk is.
+// own range and its share of the new table entries; the requests' own outputs are written by the workgroup whose turn the chunk is.
 // No workgroup waits for another: what one needs of another's table entries it takes from the free list itself.
-// Bound by the latency of a chunk's loads and two scans.
+// Bound by the latency of a chunk's loads (those of the next are on their way), two scans, a search.
 __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_each) {
-    __shared__ int64_t scratch[kPlanThreads / 64];
-    __shared__ int s_start[kPlanChunk], s_held[kPlanChunk], s_pop[kPlanChunk];     // s_pop: place in the pops, -1 of a request not admitted
+    __shared__ int scratch[2][kPlanThreads / 64];
+    __shared__ int s_start[kPlanChunk], s_held[kPlanChunk], s_entry[kPlanChunk];   // s_entry: blocks that the requests before this one ask for
+    __shared__ bool s_granted[kPlanChunk];
     const int t = threadIdx.x, block = 1 << a.block_log;
     const int64_t capacity = (int64_t)a.width << a.block_log;
-    const int count = max(0, min(*a.free_count, a.blocks));
-    const int64_t r0 = (int64_t)blockIdx.x * rows_each, r1 = min((int64_t)a.rows, r0 + rows_each);
-    int64_t rows_before = 0, need_before = 0, taken = 0;
-    auto free_block = [&](int64_t place) { return a.free_blocks[count - 1 - place]; };
-    for (int c0 = 0, chunk = 0; c0 < a.requests; c0 += kPlanChunk, ++chunk) {
-        int held[kPlanEach], fresh[kPlanEach];
-        int64_t sum = 0;
+    auto read = [&](const int32_t *p, int c0, int (&v)[kPlanEach]) {
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
             const int i = c0 + t * kPlanEach + j;
-            held[j] = i < a.requests ? a.held[i] : 0;
-            fresh[j] = i < a.requests ? a.fresh[i] : 0;
-            sum += max(fresh[j], 0);
+            v[j] = i < a.requests ? p[i] : 0;
         }
-        int64_t chunk_rows, chunk_need;
-        int64_t start[kPlanEach], need[kPlanEach];
-        int64_t at = rows_before + block_scan(sum, scratch, chunk_rows);
-        int64_t wanted = 0;
+    };
+    int held_next[kPlanEach], fresh_next[kPlanEach];
+    read(a.held, 0, held_next);
+    read(a.fresh, 0, fresh_next);
+    const int count = max(0, min(*a.free_count, a.blocks));
+    auto free_block = [&](int place) { return a.free_blocks[count - 1 - place]; };
+    const int r0 = min(blockIdx.x * (int64_t)rows_each, (int64_t)a.rows), r1 = min(r0 + rows_each, a.rows);
+    int rows_before = 0, need_before = 0, taken = 0;
+    for (int c0 = 0, chunk = 0; c0 < a.requests; c0 += kPlanChunk, ++chunk) {
+        int held[kPlanEach], fresh[kPlanEach], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPlanEach; ++j) {
+            held[j] = held_next[j];
+            fresh[j] = fresh_next[j];
+            sum = add_up(sum, max(min(fresh[j], kMany), 0));
+        }
+        if (c0 + kPlanChunk < a.requests) {
+            read(a.held, c0 + kPlanChunk, held_next);
+            read(a.fresh, c0 + kPlanChunk, fresh_next);
+        }
+        int chunk_rows, chunk_need, start[kPlanEach], need[kPlanEach], wanted = 0;
+        int at = add_up(rows_before, block_scan(sum, scratch[0], chunk_rows));
         bool fits[kPlanEach];
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
             const int64_t all = (int64_t)held[j] + fresh[j];
             start[j] = at;
-            at += max(fresh[j], 0);
+            at = add_up(at, max(min(fresh[j], kMany), 0));
             fits[j] = held[j] >= 0 && fresh[j] >= 0 && all <= capacity && at <= a.rows;
-            need[j] = fits[j] ? ((all + block - 1) >> a.block_log) - (((int64_t)held[j] + block - 1) >> a.block_log) : 0;
-            wanted += need[j];
+            need[j] = fits[j] ? (int)(((all + block - 1) >> a.block_log) - (((int64_t)held[j] + block - 1) >> a.block_log)) : 0;
+            wanted = add_up(wanted, need[j]);
         }
-        int64_t pop = need_before + block_scan(wanted, scratch, chunk_need);
+        int entry = block_scan(wanted, scratch[1], chunk_need);
         const bool mine = chunk % gridDim.x == blockIdx.x;
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
-            const int i = c0 + t * kPlanEach + j;
-            const bool granted = fits[j] && (need[j] == 0 || pop + need[j] <= count);
-            if (granted && need[j]) taken = pop + need[j];
-            s_start[t * kPlanEach + j] = (int)min(start[j], (int64_t)a.rows);
+            const int i = c0 + t * kPlanEach + j, upto = add_up(add_up(need_before, entry), need[j]);
+            const bool granted = fits[j] && (need[j] == 0 || upto <= count);
+            if (granted && need[j]) taken = upto;
+            s_start[t * kPlanEach + j] = min(start[j], a.rows);
             s_held[t * kPlanEach + j] = held[j];
-            s_pop[t * kPlanEach + j] = granted ? (int)pop : -1;
+            s_entry[t * kPlanEach + j] = entry;
+            s_granted[t * kPlanEach + j] = granted;
             if (mine && i < a.requests) {
-                a.starts[i] = (int)min(start[j], (int64_t)a.rows);
+                a.starts[i] = min(start[j], a.rows);
                 a.lengths[i] = granted ? held[j] + fresh[j] : (int)max((int64_t)0, min((int64_t)held[j], capacity));
-                if (granted) {
-                    int32_t *entry = a.table + (int64_t)i * a.width + (((int64_t)held[j] + block - 1) >> a.block_log);
-                    for (int64_t b = 0; b < need[j]; ++b) entry[b] = free_block(pop + b);
-                }
             }
-            pop += need[j];
+            entry = add_up(entry, need[j]);
         }
         __syncthreads();
-        const int64_t lo = max(r0, rows_before), hi = min(r1, rows_before + chunk_rows);
         const int last = min(kPlanChunk, a.requests - c0) - 1;
-        for (int64_t r = lo + t; r < hi; r += kPlanThreads) {
-            int i = 0;                     // the last request that starts at r or before
-            for (int step = kPlanChunk / 2; step; step /= 2)
-                if (i + step <= last && s_start[i + step] <= r) i += step;
-            const int first = s_pop[i];
+        // new table entries: a workgroup writes its share of the chunk's, up to where the free list ends
+        const int entries = max(0, min(chunk_need, count - need_before)), share = (int)(((int64_t)entries + gridDim.x - 1) / gridDim.x);
+        const int e1 = (int)min((int64_t)entries, (int64_t)share * (blockIdx.x + 1));
+        for (int64_t e = (int64_t)share * blockIdx.x + t; e < e1; e += kPlanThreads) {
+            const int i = last_from(s_entry, last, (int)e);
+            if (!s_granted[i]) continue;
+            const int column = (int)((((int64_t)s_held[i] + block - 1) >> a.block_log) + (e - s_entry[i]));
+            a.table[(int64_t)(c0 + i) * a.width + column] = free_block(need_before + (int)e);
+        }
+        const int lo = max(r0, rows_before), hi = min(r1, add_up(rows_before, chunk_rows));
+        for (int r = lo + t; r < hi; r += kPlanThreads) {
+            const int i = last_from(s_start, last, r);
             int32_t position = -1;
             int64_t slot = -1;
-            if (first >= 0) {
-                position = s_held[i] + (int)(r - s_start[i]);
-                const int b = position >> a.block_log, old = (s_held[i] + block - 1) >> a.block_log;
-                const int id = b < old ? a.table[(int64_t)(c0 + i) * a.width + b] : free_block(first + b - old);
+            if (s_granted[i]) {
+                position = s_held[i] + (r - s_start[i]);
+                const int b = position >> a.block_log, old = (int)(((int64_t)s_held[i] + block - 1) >> a.block_log);
+                const int id = b < old ? a.table[(int64_t)(c0 + i) * a.width + b] : free_block(need_before + s_entry[i] + b - old);
                 if (id >= 0 && id < a.blocks) slot = ((int64_t)id << a.block_log) + (position & (block - 1));
             }
             a.positions[r] = position;
             a.slots[r] = slot;
         }
-        rows_before += chunk_rows;
-        need_before += chunk_need;
+        rows_before = add_up(rows_before, chunk_rows);
+        need_before = add_up(need_before, chunk_need);
         __syncthreads();
     }
-    for (int64_t r = max(r0, rows_before) + t; r < r1; r += kPlanThreads) {
+    for (int r = max(r0, rows_before) + t; r < r1; r += kPlanThreads) {
         a.positions[r] = -1;
         a.slots[r] = -1;
     }
@@ -119,12 +148,12 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_eac
     // the pops end where the last admitted request's do
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) taken = max(taken, __shfl_xor(taken, s));
-    if ((t & 63) == 0) scratch[t >> 6] = taken;
+    if ((t & 63) == 0) scratch[0][t >> 6] = taken;
     __syncthreads();
     if (t) return;
-    for (int i = 1; i < kPlanThreads / 64; ++i) taken = max(taken, scratch[i]);
-    *a.left = (int)(count - taken);
-    a.starts[a.requests] = (int)min(rows_before, (int64_t)a.rows);
+    for (int i = 1; i < kPlanThreads / 64; ++i) taken = max(taken, scratch[0][i]);
+    *a.left = count - taken;
+    a.starts[a.requests] = min(rows_before, a.rows);
 }
 
 hipError_t launch_kv_plan(const PlanArgs &a, hipStream_t st) {
@@ -269,40 +298,47 @@ __device__ static inline void norm_rope8(const typename Elem<DT>::type *head, in
     for (int i = 0; i < 8; ++i) h[i] = turned[i];
 }
 
-// A thread takes eight values of a head of a row, queries first, then keys, then values; heads [first, first + heads) of them.
-// Bound by the traffic of the rows.
+// A thread takes eight values of a head of a row.  Workgroups of queries, of keys and of values are apart: the keys' float64 is then not
+// waited for by others of its wavefront.  What a thread reads is asked for before it is known whether the row is one, so that the
+// chain of loads is a position and its angles, no more.  Bound by the traffic of the rows.
 template <int DT, int DIM, bool FAST>
-__global__ __launch_bounds__(256) void qk_norm_rope(RopeArgs a, int first, int heads) {
+__global__ __launch_bounds__(256) void qk_norm_rope(RopeArgs a, uint32_t query_groups, uint32_t key_groups) {
     typedef typename Elem<DT>::type T;
-    constexpr int kLanes = DIM / 8;
-    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
-    const int64_t row = unit / heads;
-    if (row >= a.rows) return;
-    const int h = first + (int)(unit % heads), d0 = (threadIdx.x % kLanes) * 8;
-    const int position = a.positions[row];
-    const bool there = position >= 0 && (a.rotary == 0 || position < a.max_position);
-    const float *angles = a.rope + (int64_t)position * a.rotary;
-    if (h < a.q_heads) {
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (there) norm_rope8<float, DT, DIM, FAST>(static_cast<const T *>(a.q) + row * a.ldq + (int64_t)h * DIM, d0, a.q_weight, angles, a, v);
-        store8<DT>(static_cast<T *>(a.q_out) + (row * a.q_heads + h) * DIM + d0, v);
+    constexpr uint32_t kLanes = DIM / 8;
+    const uint32_t group = blockIdx.x;
+    const int d0 = (threadIdx.x % kLanes) * 8;
+    if (group < query_groups) {
+        const uint32_t unit = (group * 256 + threadIdx.x) / kLanes, row = unit / (uint32_t)a.q_heads, h = unit % (uint32_t)a.q_heads;
+        if (row >= (uint32_t)a.rows) return;
+        const int position = a.positions[row];
+        const bool there = position >= 0 && (a.rotary == 0 || position < a.max_position);
+        float v[8];
+        norm_rope8<float, DT, DIM, FAST>(static_cast<const T *>(a.q) + row * a.ldq + (int64_t)h * DIM, d0, a.q_weight,
+                                         a.rope + (there ? (int64_t)position * a.rotary : 0), a, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = there ? v[i] : 0.f;
+        store8<DT>(static_cast<T *>(a.q_out) + ((int64_t)row * a.q_heads + h) * DIM + d0, v);
         return;
     }
-    const bool key = h < a.q_heads + a.kv_heads;
-    const int hk = key ? h - a.q_heads : h - a.q_heads - a.kv_heads;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (there && key) {
+    const bool key = group < query_groups + key_groups;
+    const uint32_t unit = ((group - query_groups - (key ? 0 : key_groups)) * 256 + threadIdx.x) / kLanes;
+    const uint32_t row = unit / (uint32_t)a.kv_heads, hk = unit % (uint32_t)a.kv_heads;
+    if (row >= (uint32_t)a.rows) return;
+    const int position = a.positions[row];
+    const int64_t slot = a.cache ? a.slots[row] : -1;
+    const bool there = position >= 0 && (a.rotary == 0 || position < a.max_position);
+    float v[8];
+    if (key) {
         double x[8];
-        norm_rope8<double, DT, DIM, FAST>(static_cast<const T *>(a.k) + row * a.ldk + (int64_t)hk * DIM, d0, a.k_weight, angles, a, x);
+        norm_rope8<double, DT, DIM, FAST>(static_cast<const T *>(a.k) + row * a.ldk + (int64_t)hk * DIM, d0, a.k_weight,
+                                          a.rope + (there ? (int64_t)position * a.rotary : 0), a, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = float_odd(x[i]);
-    } else if (there) {
+        for (int i = 0; i < 8; ++i) v[i] = there ? float_odd(x[i]) : 0.f;
+        if (a.k_out) store8<DT>(static_cast<T *>(a.k_out) + ((int64_t)row * a.kv_heads + hk) * DIM + d0, v);
+    } else {
         load8<DT, FAST>(static_cast<const T *>(a.v) + row * a.ldv + (int64_t)hk * DIM + d0, v);
     }
-    if (key && a.k_out) store8<DT>(static_cast<T *>(a.k_out) + (row * a.kv_heads + hk) * DIM + d0, v);
-    if (!a.cache || !there) return;
-    const int64_t slot = a.slots[row];
-    if (slot < 0 || slot >= a.total_slots) return;
+    if (!there || slot < 0 || slot >= a.total_slots) return;
     uint32_t byte;
     const uint32_t codes = e2m1_codes8<DT>(v, byte);
     const KvLayout at{DIM, 1 << a.block_log};
@@ -318,13 +354,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope(RopeArgs a, int first, int h
 }
 
 template <int DT, int DIM> static hipError_t launch_rope_dim(const RopeArgs &a, hipStream_t st) {
-    const int first = a.q ? 0 : a.q_heads, heads = (a.q ? a.q_heads : 0) + (a.k ? (a.cache ? 2 : 1) * a.kv_heads : 0);
-    const int64_t threads = (int64_t)a.rows * heads * (DIM / 8);
+    auto groups = [&](int heads) { return (unsigned)(((int64_t)a.rows * heads * (DIM / 8) + 255) / 256); };
+    const unsigned queries = a.q ? groups(a.q_heads) : 0, keys = a.k ? groups(a.kv_heads) : 0, all = queries + keys + (a.cache ? keys : 0);
     const bool turns = a.rotary % (a.interleaved ? 8 : 16) == 0;
     const bool fast = turns && (!a.q || a.ldq % 8 == 0) && (!a.k || (a.ldk % 8 == 0 && a.ldv % 8 == 0));
-    const unsigned grid = (unsigned)((threads + 255) / 256);
-    if (fast) qk_norm_rope<DT, DIM, true><<<grid, 256, 0, st>>>(a, first, heads);
-    else qk_norm_rope<DT, DIM, false><<<grid, 256, 0, st>>>(a, first, heads);
+    if (fast) qk_norm_rope<DT, DIM, true><<<all, 256, 0, st>>>(a, queries, keys);
+    else qk_norm_rope<DT, DIM, false><<<all, 256, 0, st>>>(a, queries, keys);
     return hipGetLastError();
 }
 

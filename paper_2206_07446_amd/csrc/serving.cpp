@@ -31,6 +31,7 @@ int log2_of(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
 int check_attention(const nnv_attention_desc *d) {
     if (!d) return NNV_E_NULL;
     if (d->q_heads <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->block_tokens <= 0 || d->blocks <= 0 || d->table_blocks <= 0) return NNV_E_BAD_DESC;
+    if (d->blocks > 1 << 30) return NNV_E_BAD_DESC;
     if (d->q_heads > 1024 || d->q_heads % d->kv_heads) return NNV_E_BAD_DESC;
     if (d->rotary_dim < 0 || d->rotary_dim % 2 || d->rotary_dim > d->head_dim || (d->rotary_dim > 0 && d->positions <= 0)) return NNV_E_BAD_DESC;
     if (d->rotary_interleaved != 0 && d->rotary_interleaved != 1) return NNV_E_BAD_DESC;
@@ -109,7 +110,7 @@ int nnv_qk_norm_rope(const nnv_attention_desc *desc, int n_rows, const void *q, 
     if (const int rc = check_counts(0, n_rows)) return rc;
     if (n_rows == 0 || (!q && !k)) return NNV_OK;
     const int64_t dq = (int64_t)desc->q_heads * desc->head_dim, dk = (int64_t)desc->kv_heads * desc->head_dim;
-    if (n_rows * (dq + 2 * dk) / 2048 > kMostGroups) return NNV_E_ARG;
+    if (n_rows * (dq + 2 * dk) / 8 > INT32_MAX) return NNV_E_ARG;      // (threads are numbered in 32 bits)
     if (n_rows > 1 && ((q && ldq < dq) || (k && ldk < dk) || (k && cache && ldv < dk))) return NNV_E_ARG;
     if (!positions || (q && !q_out) || (desc->rotary_dim && !rope) || (k && !cache && !k_out) || (k && cache && (!v || !slots))) return NNV_E_NULL;
     if (off16(q) || off16(k) || off16(v) || off16(q_weight) || off16(k_weight) || off16(rope) || off4(positions) || off8(slots) || off16(q_out) ||

@@ -297,6 +297,53 @@ def test_many_rows(lengths, fresh, dim, dtype):
     Scene(layer(head_dim=dim, q_heads=4, kv_heads=2, block_tokens=16, dtype=dtype, scale=dim ** -0.5), lengths, fresh, padding=3).check()
 
 
+# rows and heads of a group enough that requests of 32 pairs and more go to the kernel for many rows, the others beside them
+MANY = [([40], [40]), ([17, 100, 260], [17, 33, 130]), ([1, 2, 300, 90, 0], [1, 2, 1, 64, 0]), ([300, 64, 65], [70, 64, 1]), ([5, 129, 1, 500], [0, 128, 1, 3])]
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, nnv.BF16), (64, nnv.F16), (128, nnv.F16), (128, nnv.BF16), (256, nnv.F16), (256, nnv.BF16)])
+@pytest.mark.parametrize("lengths,fresh", MANY, ids=str)
+def test_many_pairs(lengths, fresh, dim, dtype):
+    for heads, block in (((16, 1), 16), ((40, 2), 64)):
+        Scene(layer(head_dim=dim, q_heads=heads[0], kv_heads=heads[1], block_tokens=block, dtype=dtype, scale=dim ** -0.5), lengths, fresh, padding=3).check()
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 3), (64, 64), (100, 70), (700, 0)])
+def test_many_pairs_in_windows(window, sinks):
+    Scene(layer(q_heads=16, kv_heads=1, block_tokens=32, window=window, sinks=sinks), [40, 600, 333], [40, 50, 129], padding=1).check()
+
+
+def test_many_pairs_of_many_requests():
+    """More requests than are put in order of their lengths."""
+    g = np.random.default_rng(5)
+    lengths = [int(v) for v in g.integers(1, 150, 70)]
+    fresh = [min(n, int(v)) for n, v in zip(lengths, g.integers(0, 12, 70))]
+    Scene(layer(q_heads=16, kv_heads=2, head_dim=64, block_tokens=16), lengths, fresh, padding=2).check()
+
+
+def test_many_pairs_split_and_joined():
+    s = Scene(layer(q_heads=16, kv_heads=1, block_tokens=64, head_dim=64), [9000, 700, 40], [70, 33, 1])
+    assert nnv.nnv_kv_attention_workspace_bytes(s.d, 3, 104) > 0
+    first = s.check()
+    assert np.array_equal(first, s.run())
+
+
+def test_many_pairs_where_blocks_are_none():
+    s = Scene(layer(q_heads=16, kv_heads=1, block_tokens=16), [190, 200], [60, 40], padding=2)
+    s.positions[3] = s.positions[70] = -1
+    s.table[0][3], s.table[0][7] = -5, 10 ** 8            # tokens 48 .. 63 and 112 .. 127
+    s.table[1] = [-1] * len(s.table[1])
+    got = s.run()
+    assert (got[[3, 70]] == 0).all() and (got[60:] == 0).all()
+    s.check(got, hidden=[np.r_[48:64, 112:128], np.arange(200)])
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0])
+def test_factors_that_are_not_positive(scale):
+    for lengths, fresh in (([100, 20], [1, 1]), ([130, 20], [40, 1])):
+        Scene(layer(q_heads=16, kv_heads=1, block_tokens=16, scale=scale), lengths, fresh).check()
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (5, 0), (32, 4), (33, 33), (64, 1), (100, 40), (4096, 4), (50, 1000)])
 def test_windows(window, sinks):
     for lengths, fresh in (([1, 30, 64, 150, 500], [1, 1, 1, 1, 1]), ([30, 200], [30, 90])):
