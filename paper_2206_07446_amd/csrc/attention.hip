@@ -660,7 +660,8 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     // (what is read of splits that there are not is not used)
     const bool slot = tid < a.splits;
     const float own_base = slot ? p[tid * (DIM + kPartExtra) + DIM] : 0.f, own_sum = slot ? p[tid * (DIM + kPartExtra) + DIM + 1] : 0.f;
-    const int splits = __builtin_bit_cast(int, p[DIM + 2]);
+    // (a row that starts leave out has no partial results: what the workspace holds there may be any number)
+    const int splits = min(__builtin_bit_cast(int, p[DIM + 2]), a.splits);
     if (splits <= 1) return;
     const bool mine = tid < splits;
     const float base = mine ? own_base : -3.4028234663852886e38f;

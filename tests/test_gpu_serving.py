@@ -377,6 +377,19 @@ def test_starts_and_lengths_out_of_range_do_no_harm():
     s.run()
 
 
+def test_rows_that_starts_leave_out_beside_split_requests():
+    """Their partial results are whatever the workspace holds; the other rows are what they are without them."""
+    s = Scene(layer(q_heads=4, kv_heads=1, block_tokens=64), [9000, 33], [3, 1])
+    want = s.run()
+    s.starts = [2, 3, 4]
+    need = nnv.nnv_kv_attention_workspace_bytes(s.d, 2, 4)
+    assert need > 0
+    for word in (0x7F7F7F7F, 0x00000060, -1):
+        ws = torch.full((need // 4 + 16,), word, dtype=torch.int32, device=DEV)
+        ws[need // 4:] = -1
+        assert np.array_equal(s.run(ws.view(torch.uint8))[2:], want[2:])
+
+
 def test_positions_behind_the_length_see_what_is_held():
     s = Scene(layer(block_tokens=16), [50], [1])
     a = s.run()
