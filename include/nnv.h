@@ -398,7 +398,7 @@ int nnv_kv_read(const nnv_attention_desc *desc, int n, const int64_t *slots, con
  *   q, out : n_rows x q_heads x head_dim;  query head h reads key head h / (q_heads / kv_heads)
  *   block_table, starts, lengths, positions : as nnv_kv_plan writes them (n_requests of them, n_rows positions)
  *   workspace : >= nnv_kv_attention_workspace_bytes(desc, n_requests, n_rows) bytes, whatever its contents
- * Rows that see nothing (position below 0, no request, length 0) yield zeros.  Tokens whose table entry is no block
+ * Rows that see nothing (position below 0, no request, length 0) yield zeros; a query head that holds a NaN yields NaN.  Tokens whose table entry is no block
  * of the cache are not seen.  starts and lengths are clamped to what desc and n_rows allow; where starts do not begin at
  * 0 or do decrease, what rows that no request has yield is not defined.
  * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */

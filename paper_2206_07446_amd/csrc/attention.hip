@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             const int pr = t.pair0 + c;
             const int64_t out_row = (int64_t)(t.row0 + pr / a.group) * a.q_heads + head * a.group + pr % a.group;
             float *part = a.parts + (out_row * a.splits + split) * (DIM + kPartExtra);
-            if (whole) static_cast<T *>(a.out)[out_row * DIM + half * (DIM / 2) + d] = (T)(l > 0 ? v / l : 0.f);
+            if (whole) static_cast<T *>(a.out)[out_row * DIM + half * (DIM / 2) + d] = (T)(l == 0 ? 0.f : v / l);
             else part[half * (DIM / 2) + d] = v;
             if (half == 0 && d == 0 && a.splits > 1) {
                 part[DIM] = m;
@@ -623,7 +623,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
     // lane: pair col, values 32 d + 8 (r / 4) + 4 half + r % 4
     const int64_t out_row = (int64_t)row * a.q_heads + qh;
     float *parts = a.parts + (out_row * a.splits + split) * (DIM + kPartExtra);
-    const float inverse = sum > 0 ? 1.f / sum : 0.f;
+    const float inverse = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
     for (int d = 0; d < kD; ++d)
 #pragma unroll
@@ -688,7 +688,7 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     for (int i = 1; i < kGroups; ++i) v += part[i][at];
     ElemVec<DT, 4> y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = (T)(l > 0 ? v[i] / l : 0.f);
+    for (int i = 0; i < 4; ++i) y[i] = (T)(l == 0 ? 0.f : v[i] / l);
     *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + (int64_t)blockIdx.x * DIM + 4 * at) = y;
 }
 

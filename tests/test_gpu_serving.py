@@ -377,6 +377,20 @@ def test_starts_and_lengths_out_of_range_do_no_harm():
     s.run()
 
 
+@pytest.mark.parametrize("lengths,fresh", [([70, 33], [1, 2]), ([9000, 33], [1, 1]), ([300, 20], [70, 1]), ([9000, 40], [70, 1])], ids=str)
+def test_queries_that_are_not_numbers(lengths, fresh):
+    """A head of a row is NaN where its query holds a NaN, or an infinity (some of whose products are infinity times 0); the others are what they are."""
+    s = Scene(layer(q_heads=16, kv_heads=1, block_tokens=64, head_dim=64), lengths, fresh)
+    clean, want = s.q.clone(), s.run()
+    s.q[0, 3, 5], s.q[fresh[0], 7, 60], s.q[fresh[0], 1, 0] = float("nan"), float("inf"), -float("inf")
+    hit = np.zeros(want.shape[:2], bool)
+    hit[0, 3] = hit[fresh[0], 7] = hit[fresh[0], 1] = True
+    got = s.run()
+    assert np.isnan(got[0, 3]).all() and not np.isfinite(got[hit]).any()
+    got[hit], s.q = want[hit], clean
+    s.check(got)
+
+
 def test_rows_that_starts_leave_out_beside_split_requests():
     """Their partial results are whatever the workspace holds; the other rows are what they are without them."""
     s = Scene(layer(q_heads=4, kv_heads=1, block_tokens=64), [9000, 33], [3, 1])
