@@ -1,4 +1,5 @@
 // Host side of the serving operators declared in nnv.h: descriptors, sizes, argument checks, dispatch.
+#include <algorithm>
 #include <cmath>
 #include "nnv_internal.h"
 #include "serving.h"
@@ -156,7 +157,8 @@ int nnv_kv_attention(const nnv_attention_desc *desc, int n_requests, int n_rows,
     a.q = q; a.table = block_table; a.starts = starts; a.lengths = lengths; a.positions = positions;
     a.cache = static_cast<const char *>(cache); a.out = out;
     a.requests = n_requests; a.rows = n_rows; a.q_heads = desc->q_heads; a.kv_heads = desc->kv_heads; a.group = desc->q_heads / desc->kv_heads;
-    a.block_log = log2_of(desc->block_tokens); a.blocks = desc->blocks; a.width = desc->table_blocks; a.window = desc->window; a.sinks = desc->sinks;
+    a.block_log = log2_of(desc->block_tokens); a.blocks = desc->blocks; a.width = desc->table_blocks; a.window = desc->window;
+    a.sinks = (int)std::min((int64_t)desc->sinks, (int64_t)desc->table_blocks * desc->block_tokens);     // (no more than there can be: sums of it stay within 32 bits)
     a.scale = std::fmax(std::fabs(desc->scale) * 1.4426950408889634f, 1e-30f);
     a.flip = desc->scale < 0 ? (int)0x80008000u : 0;
     return finish(launch_kv_attention(*desc, a, workspace, static_cast<hipStream_t>(hip_stream)));

@@ -350,6 +350,13 @@ def test_windows(window, sinks):
         Scene(layer(q_heads=4, kv_heads=2, head_dim=64, block_tokens=16, window=window, sinks=sinks), lengths, fresh).check()
 
 
+@pytest.mark.parametrize("lengths,fresh", [([70, 33], [1, 2]), ([300, 20], [70, 1])], ids=str)
+def test_sinks_and_windows_of_any_size(lengths, fresh):
+    most = 2 ** 31 - 1
+    for window, sinks in ((5, most), (most, most), (most, 0)):
+        Scene(layer(q_heads=16, kv_heads=1, block_tokens=64, head_dim=64, window=window, sinks=sinks), lengths, fresh).check()
+
+
 def test_long_requests_are_split_and_joined():
     s = Scene(layer(q_heads=4, kv_heads=1, block_tokens=64), [9000, 33, 5000], [1, 1, 2])
     assert nnv.nnv_kv_attention_workspace_bytes(s.d, 3, 4) > 0
