@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
 static int attend_tiles(int requests, int rows, int group, int tile) { return (int)(((int64_t)rows * group) / tile) + requests + 1; }
 
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows) {
-    return ((int64_t)rows * (d.q_heads / d.kv_heads) / kTileRows + requests + 1) * d.kv_heads;
+    return ((int64_t)rows * (d.q_heads / d.kv_heads) / kTileRows + 2 * (int64_t)requests + 1) * d.kv_heads;
 }
 
 // Whether a request of many rows is to be expected: then both kernels run, each on the requests it is for.  (16 requests of 4 rows, group 4:
@@ -718,7 +718,7 @@ static int attend_splits(const nnv_attention_desc &d, int requests, int rows) {
     if (s > (reach + 511) / 512) s = (reach + 511) / 512;
     if (s > kMostSplits) s = kMostSplits;
     const int64_t per = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
-    while (s > 1 && (s * per > (int64_t)256 << 20 || s * kv_attention_groups(d, requests, rows) > (int64_t)1 << 30)) s = s / 2;
+    while (s > 1 && (s * per > (int64_t)256 << 20 || s * kv_attention_groups(d, requests, rows) >= 1 << 24)) s = s / 2;
     return (int)(s < 1 ? 1 : s);
 }
 

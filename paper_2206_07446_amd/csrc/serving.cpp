@@ -17,7 +17,7 @@ inline int finish(hipError_t e) { return e == hipSuccess ? NNV_OK : record_hip_e
 // Sizes that the kernels' grids can hold.
 constexpr int kMostLinearN = 1 << 22, kMostLinearK = 1 << 20, kMostLinearRows = 65535 * 16;
 constexpr int kMostRows = 1 << 24, kMostRequests = 1 << 20;
-constexpr int64_t kMostGroups = 1 << 30;
+constexpr int64_t kMostGroups = (1 << 24) - 1;        // workgroups of 256: a launch has fewer than 2^32 threads
 
 int check_linear(const nnv_linear_desc *d) {
     if (!d) return NNV_E_NULL;
@@ -125,7 +125,7 @@ int nnv_qk_norm_rope(const nnv_attention_desc *desc, int n_rows, const void *q, 
 
 int nnv_kv_read(const nnv_attention_desc *desc, int n, const int64_t *slots, const void *cache, void *k, void *v, void *hip_stream) {
     if (const int rc = check_attention(desc)) return rc;
-    if (n < 0 || n > (1 << 28) / desc->kv_heads) return NNV_E_ARG;
+    if (n < 0 || (int64_t)n * desc->kv_heads * (desc->head_dim / 8) * 2 > kMostGroups * 256) return NNV_E_ARG;
     if (n == 0 || (!k && !v)) return NNV_OK;
     if (!slots || !cache) return NNV_E_NULL;
     if (off8(slots) || off16(cache) || off16(k) || off16(v)) return NNV_E_ALIGN;

@@ -183,6 +183,9 @@ def test_read_and_attention_refusals(calls):
         assert status(f, d, 1, 1, *args, A, big) == NULL
         args[i] = A + 2
         assert status(f, d, 1, 1, *args, A, big) == ALIGN
+    # launches of 2^32 threads and more
+    assert status(nnv.nnv_kv_read, d, 1 << 26, A, A, A, A) == ARG
+    assert nnv.nnv_kv_attention_workspace_bytes(d, 1 << 19, 1 << 23) == 0 and status(f, layer(q_heads=32), 1, 1 << 24, *good, A, big) == ARG
     long = layer(table_blocks=1000)
     need = nnv.nnv_kv_attention_workspace_bytes(long, 1, 1)
     assert need > 0
