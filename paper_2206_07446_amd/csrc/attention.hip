@@ -418,20 +418,27 @@ template <> struct Mfma32<NNV_BF16> {
 // What a wavefront loads of its 16 tokens: of a lane's token and quarter of a head the key's codes, of two fours of tokens the values'.
 template <int DIM> struct HeldMany { uint32_t key[DIM / 32], key_scale, value[2][DIM / 32], value_scale[2]; };
 
-template <int DIM> __device__ static inline void load_many(const AttendArgs &a, int head, int token0, int id, HeldMany<DIM> &h) {
-    const int lane = threadIdx.x & 63, col = lane % 16, g = lane / 16;
-    const KvLayout at{DIM, 1 << a.block_log};
-    const int token = token0 & (at.tokens - 1);
-    const char *p = a.cache + ((int64_t)max(id, 0) * a.kv_heads + head) * at.head_bytes();
-    load_words(p + token * (DIM / 2) + (col * (DIM / 2) + g * (DIM / 8)), h.key);
-    const char *ks = p + (at.key_scale_at() + token * (DIM / 32)) + col * (DIM / 32);
-    if constexpr (DIM == 256) h.key_scale = *reinterpret_cast<const uint16_t *>(ks + 2 * g);
-    else h.key_scale = *reinterpret_cast<const uint8_t *>(ks + (DIM == 128 ? g : g / 2));
+// Where a lane finds these in a head's part of a block, but for the token: the rest of an address is the same for all lanes.
+template <int DIM> struct ManyPlaces {
+    uint32_t key, key_scale, key_shift, value, value_scale;      // (key_scale: of the word that the scale's byte lies in, key_shift: bits before it)
+    __device__ ManyPlaces(const KvLayout &at, uint32_t lane) {
+        const uint32_t col = lane % 16, g = lane / 16, four = g % 2;
+        key = col * (DIM / 2) + g * (DIM / 8);
+        const uint32_t byte = col * (DIM / 32) + (DIM == 256 ? 2 * g : DIM == 128 ? g : g / 2);
+        key_scale = at.key_scale_at() + byte / 4 * 4;
+        key_shift = byte % 4 * 8;
+        value = at.value_at() + (four * 16 + col) * (DIM / 8);
+        value_scale = at.value_scale_at() + (four * (DIM / 32) + col * (DIM / 16) / 32) * 4;
+    }
+};
+template <int DIM> __device__ static inline void load_many(const char *block, uint32_t token, const ManyPlaces<DIM> &at, HeldMany<DIM> &h) {
+    const uint32_t codes = token * (DIM / 2), scales = token * (DIM / 32);
+    load_words(block + (at.key + codes), h.key);
+    h.key_scale = *reinterpret_cast<const uint32_t *>(block + (at.key_scale + scales));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int four = g % 2 + 2 * k;
-        load_words(p + (at.value_at() + token * (DIM / 2)) + (four * 16 + col) * (DIM / 8), h.value[k]);
-        h.value_scale[k] = *reinterpret_cast<const uint32_t *>(p + (at.value_scale_at() + token * (DIM / 32)) + (four * (DIM / 32) + col * (DIM / 16) / 32) * 4);
+    for (int k = 0; k < 2; ++k) {                        // fours 0 or 1, then 2 or 3 of the sixteen
+        load_words(block + (at.value + codes) + k * 32 * (DIM / 8), h.value[k]);
+        h.value_scale[k] = *reinterpret_cast<const uint32_t *>(block + (at.value_scale + scales) + k * 2 * (DIM / 32) * 4);
     }
 }
 
@@ -454,19 +461,36 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
     if (split > 0 && begin >= end) return;
     const bool whole = each >= steps.count;
 
-    const TableRow table = table_row(a, t.request);
-    auto block_of = [&](int step) {                       // of the wavefront's sixteen tokens
-        const int token0 = step * kManyStep + wave * 16;
-        const int id = token0 < t.length ? table[token0 >> a.block_log] : -1;
-        return id >= 0 && id < a.blocks ? id : -1;
+    // The blocks of a step: lane l loads the entry of sixteen l % 4, through the vector unit, whose loads end in order (a scalar load on
+    // its way would make every wait for the LDS one for all).  It is asked for three steps ahead, the codes two.
+    const int32_t *table = a.table + (int64_t)t.request * a.width;
+    auto token_of = [&](int step) { return step * kManyStep + lane % 4 * 16; };
+    auto entry_at = [&](int step) { const int token = token_of(step); return table[token < t.length ? token >> a.block_log : 0]; };
+    struct Blocks { int own, here; };                     // of the wavefront's sixteen, -1: none; a bit for each sixteen that has one
+    auto blocks_at = [&](int step, int entry) {
+        const bool is = token_of(step) < t.length && (uint32_t)entry < (uint32_t)a.blocks;
+        return Blocks{__builtin_amdgcn_readlane(is ? entry : -1, wave), (int)__ballot(is) & 15};
     };
+    const KvLayout layout{DIM, 1 << a.block_log};
+    const ManyPlaces<DIM> places(layout, lane);
+    const char *head_part = a.cache + (int64_t)head * layout.head_bytes();
+    const uint32_t block_bytes = (uint32_t)a.kv_heads * layout.head_bytes();
     HeldMany<DIM> held;
-    int id = -1, next_id = -1;
+    auto load = [&](int step, int id) {
+        load_many<DIM>(head_part + (uint64_t)(uint32_t)max(id, 0) * block_bytes, (step * kManyStep + wave * 16) & (layout.tokens - 1), places, held);
+    };
     auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
+    int step = 0, step_1 = 0, step_2 = 0, entry = 0;      // this step and those after it
+    Blocks these = {-1, 0}, next = {-1, 0};               // of this step and the next
     if (begin < end) {
-        id = block_of(steps.at(begin));
-        load_many<DIM>(a, head, steps.at(begin) * kManyStep + wave * 16, id, held);
-        next_id = block_of(clamped(begin + 1));
+        step = steps.at(begin);
+        step_1 = clamped(begin + 1);
+        step_2 = clamped(begin + 2);
+        const int first = entry_at(step), second = entry_at(step_1);
+        entry = entry_at(step_2);
+        these = blocks_at(step, first);
+        next = blocks_at(step_1, second);
+        load(step, these.own);
     }
     const int i0 = wave * 32 + col, pair = t.pair0 + i0;
     const bool there = i0 < t.pairs, idle = wave * 32 >= t.pairs;
@@ -486,98 +510,90 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
         for (int r = 0; r < 16; ++r) o[d][r] = 0;
     float base = -3.4028234663852886e38f, sum = 0;
 
-    // the wavefront's sixteen tokens of a step into a buffer
-    auto spread = [&](int step, int buffer) {
-        const int c = lane % 16, g = lane / 16, h = g % 2, upper = g / 2, token0 = step * kManyStep + wave * 16;
-#pragma unroll
-        for (int i = 0; i < DIM / 32; ++i) {
-            const uint32_t byte = DIM != 256 ? held.key_scale : i >= DIM / 64 ? held.key_scale >> 8 : held.key_scale & 255;
-            const int octet_at = g * (DIM / 32) + i;
-            keys[buffer][wave / 2][octet_at / 2][octet_at % 2][wave % 2 * 16 + c] = octet<DT>(held.key[i], scale_of_byte(byte));
-        }
-        if (id < 0 || token0 + 16 > t.length) {            // what is not held may be anything: its values are to be finite, its scores are masked
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool is = id >= 0 && token0 + (h + 2 * k) * 4 + r < t.length;
-                    held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
-                }
-        }
-        uint32_t words[2][4];
-        float scale[2][4];
+    // what is not held may be anything: its values are to be finite, its scores are masked
+    auto blank = [&](int step, int id) {
+        const int g = lane / 16, h = g % 2, token0 = step * kManyStep + wave * 16;
+        if (id >= 0 && token0 + 16 <= t.length) return;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                scale[k][r] = scale_of_byte((held.value_scale[k] >> (8 * r)) & 255);
-                if constexpr (DIM == 256) words[k][r] = upper ? held.value[k][2 * r + 1] : held.value[k][2 * r];
-                else if constexpr (DIM == 128) words[k][r] = held.value[k][r] >> (16 * upper);
-                else words[k][r] = held.value[k][r / 2] >> (16 * (r % 2) + 8 * upper);
+                const bool is = id >= 0 && token0 + (h + 2 * k) * 4 + r < t.length;
+                held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
             }
-        auto pair_at = [&](int k, int r, int jj) {
-            const uint32_t w = words[k][r];
-            return (uint32_t)(jj == 0 ? Mfma<DT>::template pair<0>(w, scale[k][r]) : jj == 1 ? Mfma<DT>::template pair<1>(w, scale[k][r])
-                            : jj == 2 ? Mfma<DT>::template pair<2>(w, scale[k][r]) : Mfma<DT>::template pair<3>(w, scale[k][r]));
+    };
+    // The wavefront's sixteen tokens of a step into a buffer, in kQ pieces: eight values of a lane's key each, then halves of two values of eight tokens.
+    const int c = lane % 16, g = lane / 16, upper = g / 2;
+    i32x4_t even, odd;
+    auto spread = [&](int buffer, int piece) {
+        if (piece < kQ / 2) {
+            const uint32_t byte = (held.key_scale >> (places.key_shift + (DIM == 256 && piece >= DIM / 64 ? 8 : 0))) & 255;
+            const int octet_at = g * (DIM / 32) + piece;
+            keys[buffer][wave / 2][octet_at / 2][octet_at % 2][wave % 2 * 16 + c] = octet<DT>(held.key[piece], scale_of_byte(byte));
+            return;
+        }
+        const int jj = (piece - kQ / 2) / 2, k = piece % 2, d = c * kJ + upper * (kJ / 2) + 2 * jj;
+        auto pair_at = [&](int r) {
+            const float scale = scale_of_byte((held.value_scale[k] >> (8 * r)) & 255);
+            uint32_t w;
+            if constexpr (DIM == 256) w = upper ? held.value[k][2 * r + 1] : held.value[k][2 * r];
+            else if constexpr (DIM == 128) w = held.value[k][r] >> (16 * upper);
+            else w = held.value[k][r / 2] >> (16 * (r % 2) + 8 * upper);
+            return (uint32_t)(jj == 0 ? Mfma<DT>::template pair<0>(w, scale) : jj == 1 ? Mfma<DT>::template pair<1>(w, scale)
+                            : jj == 2 ? Mfma<DT>::template pair<2>(w, scale) : Mfma<DT>::template pair<3>(w, scale));
         };
 #pragma unroll
-        for (int jj = 0; jj < kJ / 4; ++jj) {
-            i32x4_t even, odd;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    const uint32_t x = pair_at(k, r, jj), y = pair_at(k, r + 1, jj);
-                    even[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x05040100);
-                    odd[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x07060302);
-                }
-            const int d = c * kJ + upper * (kJ / 2) + 2 * jj;
-            values[buffer][d / 32][wave][h][(d % 32) ^ (d / 16)] = even;
-            values[buffer][d / 32][wave][h][((d + 1) % 32) ^ (d / 16)] = odd;
+        for (int r = 0; r < 4; r += 2) {
+            const uint32_t x = pair_at(r), y = pair_at(r + 1);
+            even[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x05040100);
+            odd[k * 2 + r / 2] = (int)__builtin_amdgcn_perm(y, x, 0x07060302);
+        }
+        if (k) {
+            values[buffer][d / 32][wave][g % 2][(d % 32) ^ (d / 16)] = even;
+            values[buffer][d / 32][wave][g % 2][((d + 1) % 32) ^ (d / 16)] = odd;
         }
     };
-    // a bit for each sixteen of a step that is a block of the cache: scalar, the same for all wavefronts
-    auto present = [&](int step) {
-        int bits = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int token0 = step * kManyStep + i * 16;
-            const int b = token0 < t.length ? table[token0 >> a.block_log] : -1;
-            bits |= (b >= 0 && b < a.blocks ? 1 : 0) << i;
-        }
-        return bits;
-    };
-    int here = 0, here_next = 0;
     if (begin < end) {
-        here = present(steps.at(begin));
-        here_next = present(clamped(begin + 1));
-        spread(steps.at(begin), 0);
-        id = next_id;
-        load_many<DIM>(a, head, clamped(begin + 1) * kManyStep + wave * 16, id, held);
-        next_id = block_of(clamped(begin + 2));
+        blank(step, these.own);
+#pragma unroll
+        for (int d = 0; d < kQ; ++d) spread(0, d);
+        load(step_1, next.own);
     }
     __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
     __syncthreads();
     for (int i = begin; i < end; ++i) {
-        const int step = steps.at(i), buffer = (i - begin) & 1, token0 = step * kManyStep;
-        const int here_later = present(clamped(i + 2));
+        const int buffer = (i - begin) & 1, token0 = step * kManyStep;
+        blank(step_1, next.own);
+        // scores, and in the shadow of their products the next step's codes into the other buffer
+        f32x16_t s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0;
+        i32x4_t k[2][2] = {{keys[buffer][0][0][half][col], keys[buffer][1][0][half][col]}, {}};
+#pragma unroll
+        for (int d = 0; d < kQ; ++d) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                if (d + 1 < kQ) k[(d + 1) & 1][b] = keys[buffer][b][d + 1][half][col];
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = Mfma32<DT>::dot(k[d & 1][b], q[d], s[b]);
+            spread(buffer ^ 1, d);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const Blocks later = blocks_at(step_2, entry);
+        const int step_3 = clamped(i + 3);
+        entry = entry_at(step_3);
+        load(step_2, later.own);
         if (!idle && token0 <= min(wave_highest, t.length - 1)) {
-            f32x16_t s[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = 0;
-#pragma unroll
-            for (int d = 0; d < kQ; ++d)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) s[b] = Mfma32<DT>::dot(keys[buffer][b][d][half][col], q[d], s[b]);
-            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || here != 15) {
+            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || these.here != 15) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int token = token0 + b * 32 + 8 * (r / 4) + 4 * half + r % 4;
-                        const bool seen = (here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks);
+                        const bool seen = (these.here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks);
                         s[b][r] = seen ? s[b][r] : -INFINITY;
                     }
             }
@@ -610,12 +626,11 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
                 for (int d = 0; d < kD; ++d) o[d] = Mfma32<DT>::dot(values[buffer][d][k][half][col ^ (2 * d + col / 16)], weights, o[d]);
             }
         }
-        spread(clamped(i + 1), buffer ^ 1);
-        id = next_id;
-        load_many<DIM>(a, head, clamped(i + 2) * kManyStep + wave * 16, id, held);
-        next_id = block_of(clamped(i + 3));
-        here = here_next;
-        here_next = here_later;
+        these = next;
+        next = later;
+        step = step_1;
+        step_1 = step_2;
+        step_2 = step_3;
         __syncthreads();
     }
     sum += __shfl_xor(sum, 32);
