@@ -7,15 +7,13 @@ namespace nnv {
 
 // ---- the plan of a step -------------------------------------------------------------------------
 
-constexpr int kPlanThreads = 256, kPlanEach = 4, kPlanChunk = kPlanThreads * kPlanEach;
-
 // Counts are added up to kMany and no further: more than any launch has rows or any cache blocks, so that nothing wraps around.
 constexpr int kMany = 1 << 30;
 __device__ static inline int add_up(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)kMany); }
 
 // Exclusive sum over the workgroup's threads of counts of 0 to kMany; total is everybody's.  Lanes of a wavefront by shifts within rows of 16 and broadcasts
 // between those, wavefronts through the LDS (scratch, by turns one of two).
-__device__ static inline int block_scan(int v, int *scratch, int &total) {
+template <int THREADS> __device__ static inline int block_scan(int v, int *scratch, int &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int incl = v;
     incl = add_up(incl, __builtin_amdgcn_update_dpp(0, incl, 0x111, 0xf, 0xf, false));
@@ -30,7 +28,7 @@ __device__ static inline int block_scan(int v, int *scratch, int &total) {
     if (lane == 0) before = 0;
     total = 0;
 #pragma unroll
-    for (int i = 0; i < kPlanThreads / 64; ++i) {
+    for (int i = 0; i < THREADS / 64; ++i) {
         if (i < wave) before = add_up(before, scratch[i]);
         total = add_up(total, scratch[i]);
     }
@@ -38,25 +36,31 @@ __device__ static inline int block_scan(int v, int *scratch, int &total) {
 }
 
 // The last of a chunk's requests whose `from` is at `at` or before it.
-__device__ static inline int last_from(const int *from, int last, int at) {
+template <int CHUNK> __device__ static inline int last_from(const int *from, int last, int at) {
     int i = 0;
 #pragma unroll
-    for (int step = kPlanChunk / 2; step; step /= 2)
+    for (int step = CHUNK / 2; step; step /= 2)
         if (i + step <= last && from[i + step] <= at) i += step;
     return i;
 }
 
-// Every workgroup sums over all requests, 1024 at a time (two prefix sums: rows, then blocks needed), and writes the rows of its
+// Every workgroup sums over all requests, a chunk of EACH to a thread at a time (two prefix sums: rows, then blocks needed), and writes the rows of its
 // own range and its share of the new table entries; the requests' own outputs are written by the workgroup whose turn the chunk is.
 // No workgroup waits for another: what one needs of another's table entries it takes from the free list itself.
 // Bound by the latency of a chunk's loads (those of the next are on their way), two scans, a search.
-__global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_each) {
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void kv_plan(PlanArgs a, int rows_each) {
+    constexpr int kPlanThreads = THREADS, kPlanEach = EACH, kPlanChunk = kPlanThreads * EACH;
     __shared__ int scratch[2][kPlanThreads / 64];
     __shared__ int s_start[kPlanChunk], s_held[kPlanChunk], s_entry[kPlanChunk];   // s_entry: blocks that the requests before this one ask for
     __shared__ bool s_granted[kPlanChunk];
     const int t = threadIdx.x, block = 1 << a.block_log;
     const int64_t capacity = (int64_t)a.width << a.block_log;
     auto read = [&](const int32_t *p, int c0, int (&v)[kPlanEach]) {
+        if (EACH > 1 && c0 + (t + 1) * kPlanEach <= a.requests) {
+            __builtin_memcpy(v, p + c0 + t * kPlanEach, sizeof(v));
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
             const int i = c0 + t * kPlanEach + j;
@@ -83,7 +87,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_eac
             read(a.fresh, c0 + kPlanChunk, fresh_next);
         }
         int chunk_rows, chunk_need, start[kPlanEach], need[kPlanEach], wanted = 0;
-        int at = add_up(rows_before, block_scan(sum, scratch[0], chunk_rows));
+        int at = add_up(rows_before, block_scan<THREADS>(sum, scratch[0], chunk_rows));
         bool fits[kPlanEach];
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
@@ -94,7 +98,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_eac
             need[j] = fits[j] ? (int)(((all + block - 1) >> a.block_log) - (((int64_t)held[j] + block - 1) >> a.block_log)) : 0;
             wanted = add_up(wanted, need[j]);
         }
-        int entry = block_scan(wanted, scratch[1], chunk_need);
+        int entry = block_scan<THREADS>(wanted, scratch[1], chunk_need);
         const bool mine = chunk % gridDim.x == blockIdx.x;
 #pragma unroll
         for (int j = 0; j < kPlanEach; ++j) {
@@ -117,14 +121,14 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_eac
         const int entries = max(0, min(chunk_need, count - need_before)), share = (int)(((int64_t)entries + gridDim.x - 1) / gridDim.x);
         const int e1 = (int)min((int64_t)entries, (int64_t)share * (blockIdx.x + 1));
         for (int64_t e = (int64_t)share * blockIdx.x + t; e < e1; e += kPlanThreads) {
-            const int i = last_from(s_entry, last, (int)e);
+            const int i = last_from<kPlanChunk>(s_entry, last, (int)e);
             if (!s_granted[i]) continue;
             const int column = (int)((((int64_t)s_held[i] + block - 1) >> a.block_log) + (e - s_entry[i]));
             a.table[(int64_t)(c0 + i) * a.width + column] = free_block(need_before + (int)e);
         }
         const int lo = max(r0, rows_before), hi = min(r1, add_up(rows_before, chunk_rows));
         for (int r = lo + t; r < hi; r += kPlanThreads) {
-            const int i = last_from(s_start, last, r);
+            const int i = last_from<kPlanChunk>(s_start, last, r);
             int32_t position = -1;
             int64_t slot = -1;
             if (s_granted[i]) {
@@ -157,10 +161,15 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan(PlanArgs a, int rows_eac
 }
 
 hipError_t launch_kv_plan(const PlanArgs &a, hipStream_t st) {
-    // a workgroup per 1024 rows, as many as the chip holds at a time
+    // A workgroup per 1024 rows, as many as the chip holds at a time.  A request to a thread and all of them in one chunk where that can be: us with 256
+    // threads x 1, 256 x 4, 1024 x 1, x 2, x 4, of one row a request: 64 requests 4.4, 5.4, 5.6, 6.3, 7.2; 1024: 10.4, 7.7, 5.6, 6.4, 7.3;
+    // 2000: 16.3, 10.7, 8.3, 6.4, 7.5; 3000: 21.5, 13.0, 10.9, 9.7, 7.6; 9000: 55, 27, 26, 19, 16.
     const int wanted = (int)((a.rows + (int64_t)1023) / 1024), groups = wanted < 1 ? 1 : wanted > 512 ? 512 : wanted;
     const int each = (int)((a.rows + (int64_t)groups - 1) / groups);
-    kv_plan<<<groups, kPlanThreads, 0, st>>>(a, each);
+    if (a.requests <= 256) kv_plan<256, 1><<<groups, 256, 0, st>>>(a, each);
+    else if (a.requests <= 1024) kv_plan<1024, 1><<<groups, 1024, 0, st>>>(a, each);
+    else if (a.requests <= 2048) kv_plan<1024, 2><<<groups, 1024, 0, st>>>(a, each);
+    else kv_plan<1024, 4><<<groups, 1024, 0, st>>>(a, each);
     return hipGetLastError();
 }
 
@@ -193,14 +202,21 @@ template <int DIM> __device__ static inline uint32_t load_value_codes(const char
 // Eight of the 32 values of a group, four lanes to a group, -> their codes and the group's scale byte.
 template <int DT> __device__ static inline uint32_t e2m1_codes8(const float (&v)[8], uint32_t &byte) {
     float x[8];
-    uint32_t amax = 0;
+    auto most = [&] {
+        uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = e2m1_input(v[i]);
-        amax = max(amax, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
+        for (int i = 0; i < 8; ++i) amax = max(amax, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+        return max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i];
+    uint32_t amax = most();
+    if (__any(amax >= kInfBits)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = e2m1_input(x[i]);
+        amax = most();
     }
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
-    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
     byte = e2m1_scale_byte<DT>(amax);
     const float scale = scale_of_byte(byte);
     uint32_t w = 0;
@@ -211,132 +227,175 @@ template <int DT> __device__ static inline uint32_t e2m1_codes8(const float (&v)
     return w;
 }
 
-template <int DT, bool FAST> __device__ static inline void load8(const typename Elem<DT>::type *p, float (&v)[8]) {
-    if constexpr (FAST) {
-        const ElemVec<DT, 8> x = *reinterpret_cast<const ElemVec<DT, 8> *>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
-    }
-}
 __device__ static inline void load8f(const float *p, float (&v)[8]) {
     const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
 }
-template <int DT> __device__ static inline void store8(typename Elem<DT>::type *p, const float (&v)[8]) {
+// Rounded; zeros where the row is none.
+template <int DT> __device__ static inline void store8(typename Elem<DT>::type *p, const float (&v)[8], bool there = true) {
     ElemVec<DT, 8> x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (typename Elem<DT>::type)v[i];
-    *reinterpret_cast<ElemVec<DT, 8> *>(p) = x;
+    i32x4_t words = __builtin_bit_cast(i32x4_t, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) words[i] = there ? words[i] : 0;
+    *reinterpret_cast<i32x4_t *>(p) = words;
 }
 
-// Norm and rotation of values d0 .. d0 + 7 of a head in F (float for queries, double for keys), DIM / 8 lanes to a head.
-// FAST: eight values lie in one half of the rotated part, or behind it, and come in one load.
-template <typename F, int DT, int DIM, bool FAST>
-__device__ static inline void norm_rope8(const typename Elem<DT>::type *head, int d0, const float *weight, const float *angles, const RopeArgs &a, F (&h)[8]) {
-    float x[8], w[8];
-    load8<DT, FAST>(head + d0, x);
+// What norm and rotation of values d0 .. d0 + 7 of HEADS heads of a row read, eight values of the rotation's other half with their weights among them.  FAST: these lie in one
+// half of the rotated part, or behind it, and come in one load each; the head itself is read in the place of weights and angles
+// that there are not.  The first part does not wait for the row's position, so that a thread's chain of loads has two links.
+template <int DT, int DIM, bool FAST, int HEADS> struct RopeInput {
+    typedef typename Elem<DT>::type T;
+    ElemVec<DT, 8> x[HEADS], other_x[HEADS];
+    float w[8], other_w[8], cs[8], sn[8];
+    int half, other;
+    bool turns, low;
+    static __device__ ElemVec<DT, 8> eight(const T *p) {
+        if constexpr (FAST) return *reinterpret_cast<const ElemVec<DT, 8> *>(p);
+        ElemVec<DT, 8> v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = (F)x[i];
-    F inv = 1;
-    if (weight) {
-        F sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
-#pragma unroll
-        for (int s = 1; s < DIM / 8; s *= 2) sum += __shfl_xor(sum, s);
-        inv = (F)1 / sqrt(sum / (F)DIM + (F)a.eps);
-        load8f(weight + d0, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = h[i] * inv * (F)w[i];
+        for (int i = 0; i < 8; ++i) v[i] = p[i];
+        return v;
     }
-    if (d0 >= a.rotary) return;
-    const int half = a.rotary / 2;
-    F turned[8];
-    if constexpr (FAST) {
-        float c[8], s[8], o[8];
-        if (a.interleaved) {
-            const f32x4_t cc = *reinterpret_cast<const f32x4_t *>(angles + d0 / 2), ss = *reinterpret_cast<const f32x4_t *>(angles + half + d0 / 2);
+    // of heads `head`, .. `more` further ones (the last of them again where a thread takes more)
+    __device__ void load_values(const T *head, int more, int d0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                turned[2 * i] = h[2 * i] * (F)cc[i] - h[2 * i + 1] * (F)ss[i];
-                turned[2 * i + 1] = h[2 * i + 1] * (F)cc[i] + h[2 * i] * (F)ss[i];
-            }
+        for (int n = 0; n < HEADS; ++n) x[n] = eight(head + (n ? min(n, more) * DIM : 0) + d0);
+    }
+    __device__ void load_rest(const T *head, int more, int d0, const float *weight, const RopeArgs &a) {
+        half = a.rotary / 2;
+        turns = d0 < a.rotary;
+        low = d0 < half;
+        if constexpr (FAST) {
+            other = !turns || a.interleaved ? d0 : low ? d0 + half : d0 - half;
+#pragma unroll
+            for (int n = 0; n < HEADS; ++n) other_x[n] = eight(head + (n ? min(n, more) * DIM : 0) + other);
+            const float *none = reinterpret_cast<const float *>(head);
+            load8f(weight ? weight + d0 : none, w);
+            load8f(weight ? weight + other : none, other_w);
         } else {
-            const bool low = d0 < half;
-            const int other = low ? d0 + half : d0 - half, angle = low ? d0 : other;
-            load8<DT, true>(head + other, o);
-            if (weight) load8f(weight + other, w);
-            load8f(angles + angle, c);
-            load8f(angles + half + angle, s);
+            if (weight) load8f(weight + d0, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                F p = (F)o[i];
-                if (weight) p = p * inv * (F)w[i];
-                turned[i] = low ? h[i] * (F)c[i] - p * (F)s[i] : h[i] * (F)c[i] + p * (F)s[i];
+                const int d = d0 + i, at = d >= a.rotary ? d : a.interleaved ? d ^ 1 : d < half ? d + half : d - half;
+#pragma unroll
+                for (int n = 0; n < HEADS; ++n) other_x[n][i] = head[(n ? min(n, more) * DIM : 0) + at];
+                if (weight) other_w[i] = weight[at];
             }
         }
-    } else {
+    }
+    __device__ void load_angles(const T *head, int d0, const float *angles, const RopeArgs &a) {
+        if constexpr (FAST) {
+            const float *none = reinterpret_cast<const float *>(head);
+            const int angle = !turns ? 0 : a.interleaved ? d0 / 2 : low ? d0 : other, more = a.interleaved || !a.rotary ? 0 : 4;
+            const float *c = a.rotary ? angles + angle : none, *s = a.rotary ? angles + half + angle : none;
+            const f32x4_t c0 = *reinterpret_cast<const f32x4_t *>(c), c1 = *reinterpret_cast<const f32x4_t *>(c + more);
+            const f32x4_t s0 = *reinterpret_cast<const f32x4_t *>(s), s1 = *reinterpret_cast<const f32x4_t *>(s + more);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { cs[i] = c0[i]; cs[4 + i] = c1[i]; sn[i] = s0[i]; sn[4 + i] = s1[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int d = d0 + i, angle = a.interleaved ? d >> 1 : d < half ? d : d - half;
+                if (d < a.rotary) { cs[i] = angles[angle]; sn[i] = angles[half + angle]; }
+            }
+        }
+    }
+    // In F (float for queries, double for keys), DIM / 8 lanes to a head.
+    template <typename F> __device__ void norm_rope(int n, int d0, bool norm, const RopeArgs &a, F (&h)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = (F)(float)x[n][i];
+        F inv = 1;
+        if (norm) {
+            F sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += h[i] * h[i];
+#pragma unroll
+            for (int s = 1; s < DIM / 8; s *= 2) sum += __shfl_xor(sum, s);
+            inv = (F)1 / sqrt(sum / (F)DIM + (F)a.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = h[i] * inv * (F)w[i];
+        }
+        if (!turns) return;
+        if (FAST && a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const F x0 = h[2 * i], x1 = h[2 * i + 1];
+                h[2 * i] = x0 * (F)cs[i] - x1 * (F)sn[i];
+                h[2 * i + 1] = x1 * (F)cs[i] + x0 * (F)sn[i];
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int d = d0 + i;
-            turned[i] = h[i];
-            if (d >= a.rotary) continue;
-            const bool low = a.interleaved ? !(d & 1) : d < half;
-            const int other = a.interleaved ? d ^ 1 : low ? d + half : d - half;
-            const int angle = a.interleaved ? d >> 1 : low ? d : other;
-            F p = (F)(float)head[other];
-            if (weight) p = p * inv * (F)weight[other];
-            const F c = (F)angles[angle], s = (F)angles[half + angle];
-            turned[i] = low ? h[i] * c - p * s : h[i] * c + p * s;
+            if (!FAST && d >= a.rotary) continue;
+            const bool lower = FAST ? low : a.interleaved ? !(d & 1) : d < half;
+            F p = (F)(float)other_x[n][i];
+            if (norm) p = p * inv * (F)other_w[i];
+            h[i] = h[i] * (F)cs[i] + p * (F)(lower ? -sn[i] : sn[i]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = turned[i];
-}
+};
 
-// A thread takes eight values of a head of a row.  Workgroups of queries, of keys and of values are apart: the keys' float64 is then not
-// waited for by others of its wavefront.  What a thread reads is asked for before it is known whether the row is one, so that the
-// chain of loads is a position and its angles, no more.  Bound by the traffic of the rows.
+// A thread takes eight values of two query heads of a row, so that weights and angles are read once for them, or of one key or value head.  (8191 rows of
+// 32 heads of 128: queries alone 36.1 us with one head a thread, 28.7 with two, 27.9 with four, 23 at the rate of a copy; 64 rows are the same with all.)
+// Workgroups of queries, of keys and of values are apart: the keys' float64 is then not waited for by others of its wavefront.  Bound by the traffic of
+// the rows, or of a few rows by the chain of loads.
+constexpr int kQueryHeads = 2;
 template <int DT, int DIM, bool FAST>
 __global__ __launch_bounds__(256) void qk_norm_rope(RopeArgs a, uint32_t query_groups, uint32_t key_groups) {
     typedef typename Elem<DT>::type T;
     constexpr uint32_t kLanes = DIM / 8;
-    const uint32_t group = blockIdx.x;
+    uint32_t group = blockIdx.x;
     const int d0 = (threadIdx.x % kLanes) * 8;
+    auto is_there = [&](int position) { return position >= 0 && (a.rotary == 0 || position < a.max_position); };
     if (group < query_groups) {
-        const uint32_t unit = (group * 256 + threadIdx.x) / kLanes, row = unit / (uint32_t)a.q_heads, h = unit % (uint32_t)a.q_heads;
+        const uint32_t unit = (group * 256 + threadIdx.x) / kLanes, per_row = ((uint32_t)a.q_heads + kQueryHeads - 1) / kQueryHeads,
+                       row = unit / per_row, first = unit % per_row * kQueryHeads;
         if (row >= (uint32_t)a.rows) return;
-        const int position = a.positions[row];
-        const bool there = position >= 0 && (a.rotary == 0 || position < a.max_position);
-        float v[8];
-        norm_rope8<float, DT, DIM, FAST>(static_cast<const T *>(a.q) + row * a.ldq + (int64_t)h * DIM, d0, a.q_weight,
-                                         a.rope + (there ? (int64_t)position * a.rotary : 0), a, v);
+        const int position = a.positions[row], more = a.q_heads - 1 - (int)first;
+        const T *head = static_cast<const T *>(a.q) + row * a.ldq + (int64_t)first * DIM;
+        RopeInput<DT, DIM, FAST, kQueryHeads> in;
+        in.load_values(head, more, d0);
+        in.load_rest(head, more, d0, a.q_weight, a);
+        const bool there = is_there(position);
+        in.load_angles(head, d0, a.rope + (there ? (int64_t)position * a.rotary : 0), a);
+        T *out = static_cast<T *>(a.q_out) + ((int64_t)row * a.q_heads + first) * DIM + d0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = there ? v[i] : 0.f;
-        store8<DT>(static_cast<T *>(a.q_out) + ((int64_t)row * a.q_heads + h) * DIM + d0, v);
+        for (int n = 0; n < kQueryHeads; ++n) {
+            float v[8];
+            in.template norm_rope<float>(n, d0, a.q_weight != nullptr, a, v);
+            if (n == 0 || n <= more) store8<DT>(out + n * DIM, v, there);
+        }
         return;
     }
-    const bool key = group < query_groups + key_groups;
-    const uint32_t unit = ((group - query_groups - (key ? 0 : key_groups)) * 256 + threadIdx.x) / kLanes;
-    const uint32_t row = unit / (uint32_t)a.kv_heads, hk = unit % (uint32_t)a.kv_heads;
+    group -= query_groups;
+    const bool key = group < key_groups;
+    const uint32_t unit = ((key ? group : group - key_groups) * 256 + threadIdx.x) / kLanes, row = unit / (uint32_t)a.kv_heads, hk = unit % (uint32_t)a.kv_heads;
     if (row >= (uint32_t)a.rows) return;
     const int position = a.positions[row];
     const int64_t slot = a.cache ? a.slots[row] : -1;
-    const bool there = position >= 0 && (a.rotary == 0 || position < a.max_position);
+    const T *head = static_cast<const T *>(key ? a.k : a.v) + row * (key ? a.ldk : a.ldv) + (int64_t)hk * DIM;
+    RopeInput<DT, DIM, FAST, 1> in;
+    in.load_values(head, 0, d0);
+    bool there;
     float v[8];
     if (key) {
+        in.load_rest(head, 0, d0, a.k_weight, a);
+        there = is_there(position);
+        in.load_angles(head, d0, a.rope + (there ? (int64_t)position * a.rotary : 0), a);
         double x[8];
-        norm_rope8<double, DT, DIM, FAST>(static_cast<const T *>(a.k) + row * a.ldk + (int64_t)hk * DIM, d0, a.k_weight,
-                                          a.rope + (there ? (int64_t)position * a.rotary : 0), a, x);
+        in.template norm_rope<double>(0, d0, a.k_weight != nullptr, a, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = there ? float_odd(x[i]) : 0.f;
-        if (a.k_out) store8<DT>(static_cast<T *>(a.k_out) + ((int64_t)row * a.kv_heads + hk) * DIM + d0, v);
+        for (int j = 0; j < 8; ++j) v[j] = float_odd(x[j]);
+        if (a.k_out) store8<DT>(static_cast<T *>(a.k_out) + ((int64_t)row * a.kv_heads + hk) * DIM + d0, v, there);
     } else {
-        load8<DT, FAST>(static_cast<const T *>(a.v) + row * a.ldv + (int64_t)hk * DIM + d0, v);
+        there = is_there(position);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)in.x[0][j];
     }
     if (!there || slot < 0 || slot >= a.total_slots) return;
     uint32_t byte;
@@ -355,7 +414,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope(RopeArgs a, uint32_t query_g
 
 template <int DT, int DIM> static hipError_t launch_rope_dim(const RopeArgs &a, hipStream_t st) {
     auto groups = [&](int heads) { return (unsigned)(((int64_t)a.rows * heads * (DIM / 8) + 255) / 256); };
-    const unsigned queries = a.q ? groups(a.q_heads) : 0, keys = a.k ? groups(a.kv_heads) : 0, all = queries + keys + (a.cache ? keys : 0);
+    const unsigned queries = a.q ? groups((a.q_heads + kQueryHeads - 1) / kQueryHeads) : 0, keys = a.k ? groups(a.kv_heads) : 0, all = queries + keys + (a.cache ? keys : 0);
     const bool turns = a.rotary % (a.interleaved ? 8 : 16) == 0;
     const bool fast = turns && (!a.q || a.ldq % 8 == 0) && (!a.k || (a.ldk % 8 == 0 && a.ldv % 8 == 0));
     if (fast) qk_norm_rope<DT, DIM, true><<<all, 256, 0, st>>>(a, queries, keys);
