@@ -61,6 +61,9 @@ __device__ static inline int wave_max(int v) {
     return uniform(max(v, __shfl_xor(v, 32)));
 }
 
+// x / group for x below 2 x 1024: rounded up 2^21 / group times x is off by less than x * group <= 2^21 parts of 2^21.
+__device__ static inline int by_group(const AttendArgs &a, int x) { return (int)((uint32_t)x * a.group_inverse >> 21); }
+
 // A tile of a request: R consecutive pairs of a row and a query head of the group.
 struct Tile {
     int request, row0, pair0, pairs;     // first row of the request, first pair of the tile, pairs in it
@@ -449,17 +452,20 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
     __shared__ i32x4_t keys[2][2][kQ][2][32], values[2][kD][4][2][32];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 32, half = lane / 32;
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % a.many_tiles, split = rest / a.many_tiles;
-    const Tile t = a.requests < 64 ? find_longest<kManyRows>(a, u) : find_tile<kManyRows>(a, u);
+    const Tile t = a.ordered ? find_longest<kManyRows>(a, u) : find_tile<kManyRows>(a, u);
     if (t.pairs == 0 || (t.request < a.requests && t.request_pairs < kManyPairs)) return;
     // positions: of the tile for the steps, of the wavefront for its masks
-    auto position_of = [&](int i) { return i < t.pairs ? a.positions[t.row0 + (t.pair0 + i) / a.group] : -1; };
+    const int row0 = t.row0 + t.pair0 / a.group, rest0 = t.pair0 % a.group;       // row and head of the tile's first pair
+    auto position_of = [&](int i) { return i < t.pairs ? a.positions[row0 + by_group(a, rest0 + i)] : -1; };
     const int p0 = position_of(lane), p1 = position_of(lane + 64);
-    const int highest = wave_max(max(p0, p1));
-    const int seeing = -wave_max(max(p0 >= 0 ? -p0 : -0x7fffffff, p1 >= 0 ? -p1 : -0x7fffffff));
-    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length);
-    const int each = (steps.count + a.splits - 1) / a.splits, begin = split * each, end = min(steps.count, begin + each);
-    if (split > 0 && begin >= end) return;
-    const bool whole = each >= steps.count;
+    // the wavefront's queries
+    const int i0 = wave * 32 + col;
+    const bool there = i0 < t.pairs, idle = wave * 32 >= t.pairs;
+    const int row = row0 + by_group(a, rest0 + i0), qh = head * a.group + (rest0 + i0) - by_group(a, rest0 + i0) * a.group;
+    i32x4_t q[kQ];
+#pragma unroll
+    for (int s = 0; s < kQ; ++s)
+        q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + s * 16 + half * 8, a.flip) : i32x4_t{0, 0, 0, 0};
 
     // The blocks of a step: lane l loads the entry of sixteen l % 4, through the vector unit, whose loads end in order (a scalar load on
     // its way would make every wait for the LDS one for all).  It is asked for three steps ahead, the codes two.
@@ -479,30 +485,35 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
     auto load = [&](int step, int id) {
         load_many<DIM>(head_part + (uint64_t)(uint32_t)max(id, 0) * block_bytes, (step * kManyStep + wave * 16) & (layout.tokens - 1), places, held);
     };
-    auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
+    // Without a window and splits the first steps are known before the positions are, and with them the first codes: the chain of loads
+    // that a tile begins with is then one link shorter.
+    const bool early = !a.window && a.splits == 1;
+    const int held_steps = (t.length + kManyStep - 1) / kManyStep;
     int step = 0, step_1 = 0, step_2 = 0, entry = 0;      // this step and those after it
     Blocks these = {-1, 0}, next = {-1, 0};               // of this step and the next
-    if (begin < end) {
-        step = steps.at(begin);
-        step_1 = clamped(begin + 1);
-        step_2 = clamped(begin + 2);
+    auto begin_at = [&](int s0, int s1, int s2) {
+        step = s0;
+        step_1 = s1;
+        step_2 = s2;
         const int first = entry_at(step), second = entry_at(step_1);
         entry = entry_at(step_2);
         these = blocks_at(step, first);
         next = blocks_at(step_1, second);
         load(step, these.own);
-    }
-    const int i0 = wave * 32 + col, pair = t.pair0 + i0;
-    const bool there = i0 < t.pairs, idle = wave * 32 >= t.pairs;
-    const int own = position_of(i0);
-    const int row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group;
+    };
+    if (early && held_steps > 0) begin_at(0, min(1, held_steps - 1), min(2, held_steps - 1));
+    const int highest = wave_max(max(p0, p1));
+    const int seeing = -wave_max(max(p0 >= 0 ? -p0 : -0x7fffffff, p1 >= 0 ? -p1 : -0x7fffffff));
+    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length);
+    const int each = (steps.count + a.splits - 1) / a.splits, begin = split * each, end = min(steps.count, begin + each);
+    if (split > 0 && begin >= end) return;
+    const bool whole = each >= steps.count;
+    auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
+    if (!early && begin < end) begin_at(steps.at(begin), clamped(begin + 1), clamped(begin + 2));
+    const int own = __shfl(wave < 2 ? p0 : p1, wave % 2 * 32 + col);
     const int position = min(own, t.length - 1), last_sink = a.window ? own - a.window : -1;
     const int wave_lowest = -wave_max(there ? -max(own, -1) : -0x7fffffff), wave_highest = wave_max(own);
     const int full_to = min(wave_lowest, t.length - 1), full_from = a.window ? wave_highest - a.window + 1 : 0;
-    i32x4_t q[kQ];
-#pragma unroll
-    for (int s = 0; s < kQ; ++s)
-        q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + s * 16 + half * 8, a.flip) : i32x4_t{0, 0, 0, 0};
     f32x16_t o[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d)
@@ -765,6 +776,9 @@ hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &ar
     a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
     a.splits = attend_splits(d, a.requests, a.rows);
     a.parts = static_cast<float *>(ws);
+    a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
+    // the order costs a loop over the requests, and is for tiles that take many steps
+    a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
     return d.dtype == NNV_F16 ? launch_attend_type<NNV_F16>(a, d.head_dim, st) : launch_attend_type<NNV_BF16>(a, d.head_dim, st);
 }
 

@@ -58,6 +58,8 @@ struct AttendArgs {
     float *parts;
     int requests, rows, q_heads, kv_heads, group, block_log, blocks, width, window, sinks;
     int tiles, splits, many, many_tiles;       // many: requests of many rows go to a kernel of their own
+    int ordered;                               // whether that takes the tiles of the longest requests first
+    uint32_t group_inverse;                    // 2^21 / group, rounded up
     float scale;        // magnitude of the factor of the scores, times log2(e); never 0, so that a score of -infinity stays one
     int flip;           // sign bits of a pair of 16-bit values where the factor is negative
 };
