@@ -34,11 +34,14 @@ template <int DT> __device__ static inline float load_as_float(const void *p, in
     return (float)static_cast<const typename Elem<DT>::type *>(p)[i];
 }
 
-// 16 consecutive inputs of a row from `at`, `left` of which are there.
-template <int DT, bool VEC> __device__ static inline void load16(const void *p, int64_t at, int left, float (&v)[16]) {
-    if (VEC && left >= 16) {
-        const auto *q = reinterpret_cast<const ElemVec<DT, 8> *>(static_cast<const typename Elem<DT>::type *>(p) + at);
-        const ElemVec<DT, 8> a = q[0], b = q[1];
+// 16 consecutive inputs of a row from `at`, `left` of which are there.  Rows may begin anywhere: loads and stores of 16 bytes need no alignment (6 rows
+// of 842 by 5376: 14.4 us with a load for each input, 8.4 so).
+template <int DT> __device__ static inline void load16(const void *p, int64_t at, int left, float (&v)[16]) {
+    if (left >= 16) {
+        const auto *q = static_cast<const typename Elem<DT>::type *>(p) + at;
+        ElemVec<DT, 8> a, b;
+        __builtin_memcpy(&a, q, sizeof(a));
+        __builtin_memcpy(&b, q + 8, sizeof(b));
 #pragma unroll
         for (int i = 0; i < 8; ++i) { v[i] = (float)a[i]; v[8 + i] = (float)b[i]; }
         return;
@@ -71,7 +74,7 @@ __device__ static inline int code_at(int row, int part) { return (part & 1) * 51
 
 // x -> codes and scales.  A workgroup takes 16 rows x 2 blocks, 8 threads a row's block: a wavefront reads 256-byte runs of 8
 // rows and writes 128-byte runs of two pieces.  Bound by the traffic of x.
-template <int DT, bool VEC>
+template <int DT>
 __global__ __launch_bounds__(256) void linear_quantise(const void *__restrict__ x, int64_t ldx, int m, int k, char *__restrict__ codes,
                                                        char *__restrict__ scales) {
     const int t = threadIdx.x, part = t & 7, r = (t >> 3) & 15, kblocks = (k + 127) / 128, held = (kblocks + 1) / 2 * 2;
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(256) void linear_quantise(const void *__restrict__ 
     if (row >= m) return;                                  // the 8 threads of a row's block leave together
     float v[16];
     const int at = kb * 128 + part * 16;
-    load16<DT, VEC>(x, row * ldx + at, k - at, v);
+    load16<DT>(x, row * ldx + at, k - at, v);
     uint32_t amax = amax_bits16(v);
     amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
     amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(256) void linear_quantise(const void *__restrict__ 
 }
 
 // Raw weights -> codes and scales, a block of 128 x 128 a workgroup.  Bound by the traffic of the raw weights.
-template <int DT, bool VEC>
+template <int DT>
 __global__ __launch_bounds__(256) void linear_pack(const void *__restrict__ w, int n, int k, char *__restrict__ codes, char *__restrict__ scales) {
     const int t = threadIdx.x, part = t & 7, r = t >> 3, kblocks = (k + 127) / 128, held = (kblocks + 1) / 2 * 2;
     const int kb = blockIdx.x, nb = blockIdx.y, at = kb * 128 + part * 16;
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(256) void linear_pack(const void *__restrict__ w, i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = nb * 128 + i * 32 + r;
-        load16<DT, VEC>(w, (int64_t)row * k + at, row < n ? k - at : 0, v[i]);
+        load16<DT>(w, (int64_t)row * k + at, row < n ? k - at : 0, v[i]);
         amax = max(amax, amax_bits16(v[i]));
     }
     for (int s = 1; s < 64; s *= 2) amax = max(amax, (uint32_t)__shfl_xor((int)amax, s));
@@ -135,11 +138,11 @@ struct LinearArgs {
 template <int DT> __device__ static inline void store4(const LinearArgs &a, int64_t row, int col, f32x4_t v) {
     if (row >= a.m || col >= a.n) return;
     typename Elem<DT>::type *y = static_cast<typename Elem<DT>::type *>(a.y) + row * a.ldy + col;
-    if (a.ldy % 4 == 0 && col + 4 <= a.n) {              // y is 16-byte aligned, col a multiple of 4
+    if (col + 4 <= a.n) {
         ElemVec<DT, 4> out;
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = (typename Elem<DT>::type)(v[i] + (a.bias ? a.bias[col + i] : 0.f));
-        *reinterpret_cast<ElemVec<DT, 4> *>(y) = out;
+        __builtin_memcpy(y, &out, sizeof(out));
         return;
     }
 #pragma unroll
@@ -148,14 +151,14 @@ template <int DT> __device__ static inline void store4(const LinearArgs &a, int6
 }
 
 template <int DT> __device__ static inline void store8(const LinearArgs &a, int64_t row, int col, f32x4_t lo, f32x4_t hi) {
-    if (DT != NNV_F32 && a.ldy % 8 == 0 && col + 8 <= a.n && row < a.m) {
+    if (DT != NNV_F32 && col + 8 <= a.n && row < a.m) {
         ElemVec<DT, 8> out;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             out[i] = (typename Elem<DT>::type)(lo[i] + (a.bias ? a.bias[col + i] : 0.f));
             out[4 + i] = (typename Elem<DT>::type)(hi[i] + (a.bias ? a.bias[col + 4 + i] : 0.f));
         }
-        *reinterpret_cast<ElemVec<DT, 8> *>(static_cast<typename Elem<DT>::type *>(a.y) + row * a.ldy + col) = out;
+        __builtin_memcpy(static_cast<typename Elem<DT>::type *>(a.y) + row * a.ldy + col, &out, sizeof(out));
         return;
     }
     store4<DT>(a, row, col, lo);
@@ -194,19 +197,14 @@ __device__ static inline float scale_at(uint32_t word, int kb) { return scale_of
 // The conversions cost nothing here, where the weights' traffic is what bounds.
 // 32 consecutive inputs of a row as words of their storage type; `left` of them are there.
 template <int DX> struct Inputs32 { uint32_t word[DX == NNV_F32 ? 32 : 16]; };
-template <int DX, bool VEC> __device__ static inline void load32(const void *p, int64_t at, int left, Inputs32<DX> &v) {
+template <int DX> __device__ static inline void load32(const void *p, int64_t at, int left, Inputs32<DX> &v) {
     typedef typename Elem<DX>::type T;
     constexpr int kWords = DX == NNV_F32 ? 32 : 16, kEach = 32 / kWords;
     const T *q = static_cast<const T *>(p) + at;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) v.word[i] = 0;
-    if (VEC && left >= 32) {
-#pragma unroll
-        for (int i = 0; i < kWords; i += 4) {
-            const i32x4_t w = reinterpret_cast<const i32x4_t *>(q)[i / 4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v.word[i + j] = (uint32_t)w[j];
-        }
+    if (left >= 32) {
+        __builtin_memcpy(v.word, q, sizeof(v.word));
     } else if (left > 0) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -266,7 +264,7 @@ template <int DX> __device__ static inline i32x8_t codes32(const Inputs32<DX> &v
 }
 
 constexpr int kRowWaves = 8;
-template <int DT, int DX, bool VEC, int NT>
+template <int DT, int DX, int NT>
 __global__ __launch_bounds__(64 * kRowWaves) void linear_rows(LinearArgs a, const void *__restrict__ x, int64_t ldx, int k) {
     constexpr int kAhead = NT == 1 ? 4 : 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), words = (a.kblocks + 3) / 4, tile = blockIdx.x * NT;
@@ -284,7 +282,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void linear_rows(LinearArgs a, cons
     };
     auto fetch_inputs = [&](int kb, Inputs32<DX> &v) {
         const int at = kb * 128 + quarter * 32;
-        load32<DX, VEC>(x, row * ldx + at, row < a.m ? k - at : 0, v);
+        load32<DX>(x, row * ldx + at, row < a.m ? k - at : 0, v);
     };
     const int last = a.kblocks - 1;                      // behind it, it is loaded again (see linear_waves)
 #pragma unroll
@@ -633,12 +631,12 @@ static LinearPlan linear_plan(const nnv_linear_desc &d, int m) {
     return {kWaves, parts(count(32, 64), 2048)};
 }
 
-template <int DT, int DX, bool VEC> static hipError_t launch_rows(const LinearArgs &a, const void *x, int64_t ldx, int k, hipStream_t st) {
+template <int DT, int DX> static hipError_t launch_rows(const LinearArgs &a, const void *x, int64_t ldx, int k, hipStream_t st) {
     // As many outputs to a workgroup as leave three workgroups to four compute units.  Four rows, us with 16, 32, 64 outputs:
     // n 4096, k 8192: 11.8, 12.3, 14.5;  6144, 4096: 10.3, 8.9, 9.2;  8192, 8192: 19.6, 15.1, 18.4;  12288, 4096: 17.9, 15.9, 12.6
-    if (a.n >= 192 * 64) linear_rows<DT, DX, VEC, 4><<<(a.n + 63) / 64, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
-    else if (a.n >= 192 * 32) linear_rows<DT, DX, VEC, 2><<<(a.n + 31) / 32, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
-    else linear_rows<DT, DX, VEC, 1><<<(a.n + 15) / 16, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
+    if (a.n >= 192 * 64) linear_rows<DT, DX, 4><<<(a.n + 63) / 64, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
+    else if (a.n >= 192 * 32) linear_rows<DT, DX, 2><<<(a.n + 31) / 32, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
+    else linear_rows<DT, DX, 1><<<(a.n + 15) / 16, 64 * kRowWaves, 0, st>>>(a, x, ldx, k);
     return hipGetLastError();
 }
 
@@ -657,15 +655,13 @@ template <int DT> static hipError_t launch_product(const LinearArgs &a, LinearWa
 
 template <int DT> static hipError_t launch_quantise(const void *x, int64_t ldx, int m, int k, char *codes, char *scales, hipStream_t st) {
     const dim3 grid((blocks128(k) + 1) / 2, (m + 15) / 16);
-    if (ldx * (int64_t)sizeof(typename Elem<DT>::type) % 16 == 0) linear_quantise<DT, true><<<grid, 256, 0, st>>>(x, ldx, m, k, codes, scales);
-    else linear_quantise<DT, false><<<grid, 256, 0, st>>>(x, ldx, m, k, codes, scales);
+    linear_quantise<DT><<<grid, 256, 0, st>>>(x, ldx, m, k, codes, scales);
     return hipGetLastError();
 }
 
 template <int DT> static hipError_t launch_pack(const void *w, int n, int k, char *codes, char *scales, hipStream_t st) {
     const dim3 grid(held_blocks(k), blocks128(n));
-    if (k * sizeof(typename Elem<DT>::type) % 16 == 0) linear_pack<DT, true><<<grid, 256, 0, st>>>(w, n, k, codes, scales);
-    else linear_pack<DT, false><<<grid, 256, 0, st>>>(w, n, k, codes, scales);
+    linear_pack<DT><<<grid, 256, 0, st>>>(w, n, k, codes, scales);
     return hipGetLastError();
 }
 
@@ -698,9 +694,8 @@ hipError_t launch_linear(const nnv_linear_desc &d, int m, const void *x, int64_t
     const LinearPlan plan = linear_plan(d, m);
     a.splits = plan.splits;
     a.parts = reinterpret_cast<float *>(codes + linear_x_bytes(m, d.k));
-    if (plan.way == kRows) return with_type(d.y_dtype, [&](auto dt) { return with_type(d.x_dtype, [&](auto dx) { 
-        const bool lines = ldx * (int64_t)sizeof(typename Elem<dx.value>::type) % 16 == 0;
-        return lines ? launch_rows<dt.value, dx.value, true>(a, x, ldx, d.k, st) : launch_rows<dt.value, dx.value, false>(a, x, ldx, d.k, st); }); });
+    if (plan.way == kRows)
+        return with_type(d.y_dtype, [&](auto dt) { return with_type(d.x_dtype, [&](auto dx) { return launch_rows<dt.value, dx.value>(a, x, ldx, d.k, st); }); });
     const hipError_t e = with_type(d.x_dtype, [&](auto dx) { return launch_quantise<dx.value>(x, ldx, m, d.k, codes, scales, st); });
     if (e != hipSuccess) return e;
     return with_type(d.y_dtype, [&](auto dt) { return launch_product<dt.value>(a, plan.way, st); });
