@@ -449,6 +449,9 @@ template <int DT, int DIM>
 __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(AttendArgs a) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 16, kJ = DIM / 16, kD = DIM / 32;
+    // Which part of a step goes before other wavefronts' work (4 prompts of 1024 rows, 4096 pairs each: heads of 64 scores 241 us, weights and outputs 262,
+    // neither 256; of 128 210, 205, 208; of 256 362 all).
+    constexpr bool kScoresFirst = DIM == 64;
     __shared__ i32x4_t keys[2][2][kQ][2][32], values[2][kD][4][2][32];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 32, half = lane / 32;
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % a.many_tiles, split = rest / a.many_tiles;
@@ -581,6 +584,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0;
+        if (kScoresFirst) __builtin_amdgcn_s_setprio(1);
         i32x4_t k[2][2] = {{keys[buffer][0][0][half][col], keys[buffer][1][0][half][col]}, {}};
 #pragma unroll
         for (int d = 0; d < kQ; ++d) {
@@ -593,6 +597,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
             spread(buffer ^ 1, d);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (kScoresFirst) __builtin_amdgcn_s_setprio(0);
         const Blocks later = blocks_at(step_2, entry);
         const int step_3 = clamped(i + 3);
         entry = entry_at(step_3);
@@ -608,6 +613,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
                         s[b][r] = seen ? s[b][r] : -INFINITY;
                     }
             }
+            if (!kScoresFirst) __builtin_amdgcn_s_setprio(1);
             float top = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
@@ -637,6 +643,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
                 for (int d = 0; d < kD; ++d) o[d] = Mfma32<DT>::dot(values[buffer][d][k][half][col ^ (2 * d + col / 16)], weights, o[d]);
             }
         }
+        if (!kScoresFirst) __builtin_amdgcn_s_setprio(0);
         these = next;
         next = later;
         step = step_1;
