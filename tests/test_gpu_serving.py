@@ -85,6 +85,57 @@ def test_plan_of_many_requests(n, share):
     run_plan(held, fresh, order, count, table, block, sum(need) + count, sum(fresh) + 5)
 
 
+@pytest.mark.parametrize("n,share", [(2048, 1.0), (2049, 1.0), (4096, 0.5), (4097, 1.0), (9001, 0.7), (9001, 1.0)])
+def test_plan_of_thousands_of_requests(n, share):
+    """One chunk of requests filled, one more than that, and several."""
+    g = np.random.default_rng(n)
+    block, width = 16, 6
+    held = [int(v) for v in g.integers(0, 60, n)]
+    fresh = [int(v) for v in np.where(g.random(n) < 0.9, 1, g.integers(0, 30, n))]
+    need = [-(-h // block) for h in held]
+    new = sum(-(-(h + f) // block) for h, f in zip(held, fresh)) - sum(need)
+    count = int(share * new)
+    order = list(map(int, g.permutation(sum(need) + count)))
+    table = [[order.pop() for _ in range(k)] + [-1] * (width - k) for k in need]
+    run_plan(held, fresh, order, count, table, block, sum(need) + count, sum(fresh))
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (3, 1), (7, 7)], ids=str)
+@pytest.mark.parametrize("norm", [True, False])
+def test_norm_rope_of_odd_heads(heads, norm):
+    """Heads that are no multiple of those a thread takes, rotations of half a head in pairs, rows of any stride."""
+    d = layer(q_heads=heads[0], kv_heads=heads[1], rotary_dim=64, rotary_interleaved=1, positions=50, block_tokens=16, blocks=4)
+    g = torch.Generator().manual_seed(11)
+    rows, (q, kv) = 33, heads
+    for stride in ((q + 2 * kv) * 128, (q + 2 * kv) * 128 + 3):
+        x = torch.randn(rows, stride, generator=g).to(torch.bfloat16)
+        weight = 1 + 0.2 * torch.randn(2, 128, generator=g)
+        table, pos = angles(50, 64), torch.randint(50, (rows,), generator=g).tolist()
+        out = torch.full((rows + 1, q, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        out_k = torch.full((rows + 1, kv, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        # each part from the start of a buffer of its own, so that a stride of any size keeps it aligned
+        parts = [p.contiguous() for p in (x, x[:, q * 128:], x[:, (q + kv) * 128:])]
+        on = [p.to(DEV) for p in parts]
+        w = [t.to(DEV) if norm else None for t in weight]
+        cache = torch.zeros(nnv.nnv_kv_cache_bytes(d), dtype=torch.uint8, device=DEV)
+        print(f"case rope heads={heads} norm={norm} stride={stride}", flush=True)
+        nnv.nnv_qk_norm_rope(d, rows, on[0], on[0].stride(0), on[1], on[1].stride(0), on[2], on[2].stride(0), *w, table.to(DEV), ints(pos), ints(list(range(rows)), torch.int64),
+                             out, out_k, cache)
+        torch.cuda.synchronize()
+        assert (out[-1] == 7).all() and (out_k[-1] == 7).all()
+        u = torch.finfo(torch.bfloat16).eps / 2
+        for got, part, n, wt, steps in ((out, parts[0], q, weight[0], 64 + 12), (out_k, parts[1], kv, weight[1], 0)):
+            ref, size = OS.norm_rope(part[:, : n * 128].double().numpy().reshape(rows, n, 128), wt.double().numpy() if norm else None, d.eps,
+                                     table.double().numpy()[pos], 64, True)
+            # queries: float32 (see above); keys: float64, of which the float32 of odd last bit is off by a step of 2^-23 at most
+            bound = (steps * 2.0 ** -24 + 2.0 ** -23) * size * (1 + 2.0 ** -6) + u * (1 + 2.0 ** -6) * np.abs(ref) + 1e-37
+            assert (np.abs(got[:-1].double().cpu().numpy() - ref) <= bound).all()
+        held = [torch.empty(rows, kv, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        nnv.nnv_kv_read(d, rows, ints(list(range(rows)), torch.int64), cache, *held)
+        v = parts[2][:, : kv * 128].double().numpy().reshape(rows, kv, 128)
+        assert np.array_equal(held[1].double().cpu().numpy(), OS.round_head(v, False))
+
+
 # ---- norms, rotations, append -------------------------------------------------------------------
 
 def angles(positions, rotary, seed=2):
