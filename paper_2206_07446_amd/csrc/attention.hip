@@ -108,7 +108,7 @@ template <int R> __device__ static inline Tile find_tile(const AttendArgs &a, in
 }
 
 // Tile u of up to 63 requests with those of the longest requests first, and of each the last: every lane adds up the tiles of the
-// requests before its own.  The tiles that take longest then begin first, and the end of a launch is not theirs (4 prompts of 1024 rows over 1024 to
+// requests before its own.  The tiles that take longest then begin first, and the end of a launch is not theirs (4 prompts of 1024 rows over 876 to
 // 6000 tokens: see kv_attend_many).
 template <int R> __device__ static inline Tile find_longest(const AttendArgs &a, int u) {
     const int lane = threadIdx.x & 63;
@@ -217,6 +217,8 @@ template <int DIM> __device__ static inline void load_step(const AttendArgs &a, 
 
 constexpr int kPartExtra = 4;      // floats of a partial result behind its values: base, sum, number of splits
 
+// Bound by memory where there is much to read (64 rows over up to 8192 tokens, 287 MB: 71 us, 4.0 TB/s, what a reduction reaches), and by the chain
+// of starts, table and codes where there is little (one row over 32768 tokens, 36 MB: 16 us).
 // One (tile, key/value head, split): its wavefronts take steps in turn, each with a softmax of its own, and are joined in the LDS.  The next
 // step's loads are in flight while one is computed, the block numbers of the one after that too.
 //
@@ -404,6 +406,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
 // that are on their way meanwhile.  Keys lie there as [32 tokens][16 values][8 of them][token], values as [32 values][16 tokens][8 of them][value],
 // every 16 bytes a lane's part of an operand.  The four lanes' worth of a token's values that a lane has in hand go to rows that lie 8 apart;
 // the row is xor-ed with its sixteen, so that they meet different banks, and reading does so as well.
+// The conversions run beside the scores' products, the exponentials beside the outputs'.  4 prompts of 1024 rows over 876 to 6000 tokens, 32 heads of
+// 128 and 8 of keys: 203-212 us, 0.93-0.97 PFLOP/s of what the rows see; vector instructions take 60 % of a compute unit's busy time, matrix ones 47 %,
+// and two workgroups that do not wait for one another are what lets them overlap (one of eight wavefronts for 256 pairs, with half the
+// conversions: 327 us).
 constexpr int kManyStep = 64, kManyRows = 128;
 
 template <int DT> struct Mfma32;
@@ -732,7 +738,8 @@ int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows)
 }
 
 // Whether a request of many rows is to be expected: then both kernels run, each on the requests it is for.  (16 requests of 4 rows, group 4:
-// 18 us by kv_attend, 21 with a launch beside it that finds nothing; 4 requests of 1024 rows: 387 us by kv_attend, 323 by both.)
+// 18 us by kv_attend, 21 with a launch beside it that finds nothing; 4 requests of 1024 rows: 412 us by kv_attend alone, 203 by both; 80 requests
+// of 15 rows, group 4: 218 and 212.)
 static bool attend_many(const nnv_attention_desc &d, int requests, int rows) { return (int64_t)(rows - requests) * (d.q_heads / d.kv_heads) >= 512; }
 
 // Splits of a tile's tokens, from what the host knows: 1024 workgroups where there are that few (four to a compute unit; with 512 to 4096 one
