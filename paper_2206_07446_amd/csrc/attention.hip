@@ -742,18 +742,19 @@ int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows)
 // of 15 rows, group 4: 218 and 212.)
 static bool attend_many(const nnv_attention_desc &d, int requests, int rows) { return (int64_t)(rows - requests) * (d.q_heads / d.kv_heads) >= 512; }
 
-// Splits of a tile's tokens, from what the host knows: 1024 workgroups where there are that few (four to a compute unit; with 512 to 4096 one
-// request of 32768 tokens and 8 heads takes the same 20 us), of at least 512 tokens (with 256 it takes 24 us, more partial
-// results to join), at most 2048 of them, or 8192 where there are tiles enough, within 256 MB of partial results.
+// Splits of a tile's tokens, from what the host knows: 1024 workgroups where there are that few (four to a compute unit), or 512 of up to 8 tiles of rows,
+// which end together or have the chip to themselves (with 1024: 4 requests of up to 16000 tokens and 8 heads 22.5 us, 18.5 so; 8 of up to 12000 and 4 heads of 256
+// 28.7, 23.1 so; but 16 requests of 8 rows, up to 4096 tokens and 8 heads 32 us with 1024, 36 with 512); of at least 512 tokens (with 256 one request of 32768 tokens and
+// 8 heads takes 26 us, more partial results to join, against 20), at most 2048 of them, or 8192 where there are tiles enough, within 256 MB of partial results.
 static int attend_splits(const nnv_attention_desc &d, int requests, int rows) {
     const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens;
     const int64_t reach = d.window && (int64_t)d.window + d.sinks < capacity ? (int64_t)d.window + d.sinks : capacity;
     const bool many = attend_many(d, requests, rows);
     const int64_t pairs = (int64_t)rows * (d.q_heads / d.kv_heads), least = requests < rows ? requests : rows;
     const int64_t full = pairs / (many ? kManyRows : kTileRows), tiles = full > least ? full : least;
-    const int64_t groups = (tiles > 0 ? tiles : 1) * d.kv_heads, fill = many ? 512 : 1024;
+    const int64_t groups = (tiles > 0 ? tiles : 1) * d.kv_heads, fill = many || tiles <= 8 ? 512 : 1024;
     int64_t s = (fill + groups - 1) / groups;
-    const int64_t longest = groups >= 2 * fill || many ? 8192 : 2048;
+    const int64_t longest = groups >= 2048 || many ? 8192 : 2048;
     if (s < (reach + longest - 1) / longest) s = (reach + longest - 1) / longest;
     if (s > (reach + 511) / 512) s = (reach + 511) / 512;
     if (s > kMostSplits) s = kMostSplits;
