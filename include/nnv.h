@@ -394,7 +394,8 @@ int nnv_kv_read(const nnv_attention_desc *desc, int n, const int64_t *slots, con
 
 /* Attention of a step's rows over the cache: for every row of request i at position p, softmax over the tokens j <= p of the
  * request (j < lengths[i]; with a window: p - j < window or j < sinks) of scale * q . k[j], times v[j].  Scores, softmax and sums are
- * float32; weights are rounded to desc.dtype for the matrix cores.
+ * float32; weights are rounded to desc.dtype for the matrix cores: by half a step each, and in float16 by up to 2^-35 of a row's largest where they
+ * lie below 2^-24 of it.
  *   q, out : n_rows x q_heads x head_dim;  query head h reads key head h / (q_heads / kv_heads)
  *   block_table, starts, lengths, positions : as nnv_kv_plan writes them (n_requests of them, n_rows positions)
  *   workspace : >= nnv_kv_attention_workspace_bytes(desc, n_requests, n_rows) bytes, whatever its contents

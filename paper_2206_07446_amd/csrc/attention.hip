@@ -46,6 +46,13 @@ template <int DT> __device__ static inline i32x4_t octet(uint32_t w, float scale
                    Mfma<DT>::template pair<3>(w, scale)};
 }
 
+// Weights as they are rounded for the products, in powers of two: what the largest is given when a column's base is raised, and the most that one may be before
+// it is raised again.  bfloat16 has float32's exponents.  float16's numbers end at 2^16, and those below 2^-14 have fewer bits: with the largest at 2^10
+// or more, a weight keeps all its bits down to 2^-24 of the largest, and is off by 2^-35 of that at most below; thousands of tokens beside one that lies far above
+// them then count for what they are.
+template <int DT> struct WeightRange { static constexpr float kTop = 0, kMost = 8; };
+template <> struct WeightRange<NNV_F16> { static constexpr float kTop = 10, kMost = 15; };
+
 // Over the 16 lanes of a row, everywhere.
 __device__ static inline int row_max(int v) {
     v = max(v, __builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, false));      // lanes xor 1
@@ -223,8 +230,8 @@ constexpr int kPartExtra = 4;      // floats of a partial result behind its valu
 // step's loads are in flight while one is computed, the block numbers of the one after that too.
 //
 // A column's scores are taken relative to a base that all its lanes share.  It need not be the maximum: it is raised,
-// and what was summed is scaled down, only when a score of the wavefront lies 2^8 above it, which past the
-// first steps is hardly ever; weights up to 2^8 cost the sums in float32 and the rounding to 16 bits nothing.
+// and what was summed is scaled down, only when a weight of the wavefront would pass the most of WeightRange, which past the
+// first steps is hardly ever.
 template <int DT, int DIM>
 __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_attend(AttendArgs a) {
     typedef typename Elem<DT>::type T;
@@ -311,10 +318,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
                 }
         }
         float top = a.scale * fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-        if (__any(top > base + 8.f)) {
+        if (__any(top > base + WeightRange<DT>::kMost)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(base, top), keep = __builtin_amdgcn_exp2f(base - now);
+            const float now = fmaxf(base, top - WeightRange<DT>::kTop), keep = __builtin_amdgcn_exp2f(base - now);
             base = now;
             sum *= keep;
 #pragma unroll
@@ -624,9 +631,9 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
 #pragma unroll
             for (int e = 0; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
             top *= a.scale;
-            if (__any(top > base + 8.f)) {
+            if (__any(top > base + WeightRange<DT>::kMost)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(base, top), keep = __builtin_amdgcn_exp2f(base - now);
+                const float now = fmaxf(base, top - WeightRange<DT>::kTop), keep = __builtin_amdgcn_exp2f(base - now);
                 base = now;
                 sum *= keep;
 #pragma unroll
