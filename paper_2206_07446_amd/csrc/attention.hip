@@ -53,6 +53,21 @@ template <int DT> __device__ static inline i32x4_t octet(uint32_t w, float scale
 template <int DT> struct WeightRange { static constexpr float kTop = 0, kMost = 8; };
 template <> struct WeightRange<NNV_F16> { static constexpr float kTop = 10, kMost = 15; };
 
+// The base that a largest score asks for; where float32 has no number kTop below it, none that gives a weight of more than kMost.
+template <int DT> __device__ static inline float raised(float base, float top) {
+    const float now = fmaxf(base, top - WeightRange<DT>::kTop);
+    return top - now > WeightRange<DT>::kMost ? top : now;
+}
+// Scores in powers of two have their product with the factor rounded before the base is taken off, so that the largest is its base's own however large it is: in
+// one instruction with that, which sees the product unrounded, the two are apart by half a step of float32 at that size, more than a weight can stand from 2^24 or so.
+__device__ static inline float in_twos(float score, float scale) {
+#pragma clang fp contract(off)
+    return score * scale;
+}
+// kv_attend_many, where vector instructions count (4 prompts of 1024 rows 134 -> 155 us with heads of 64, 213 -> 222 with 128), does that only for bases beyond 2^12
+// (but not for that of a column that has seen nothing): up to there the two are 2^-13 apart, and no rounding to 16 bits sees it.
+__device__ static inline bool far_out(float base) { return __any(fabsf(base) > 0x1p12f && base > -3e38f); }
+
 // Over the 16 lanes of a row, everywhere.
 __device__ static inline int row_max(int v) {
     v = max(v, __builtin_amdgcn_update_dpp(v, v, 0xb1, 0xf, 0xf, false));      // lanes xor 1
@@ -299,7 +314,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
         }
         float p[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4];
+        for (int e = 0; e < 8; ++e) p[e] = in_twos(s[e / 4][e % 4], a.scale);
         const int token0 = step * kStep;
         if (token0 + kStep - 1 > full_to || (token0 < full_from && token0 + kStep > a.sinks) || blocks.id[0] < 0 || blocks.id[1] < 0) {
 #pragma unroll
@@ -317,18 +332,18 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
                     held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
                 }
         }
-        float top = a.scale * fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-        if (__any(top > base + WeightRange<DT>::kMost)) {
+        float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+        if (__any(top - base > WeightRange<DT>::kMost)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(base, top - WeightRange<DT>::kTop), keep = __builtin_amdgcn_exp2f(base - now);
+            const float now = raised<DT>(base, top), keep = __builtin_amdgcn_exp2f(base - now);
             base = now;
             sum *= keep;
 #pragma unroll
             for (int j = 0; j < kJ; ++j) o[j] *= keep;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale, -base));
+        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(p[e] - base);
         sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         const i32x4_t weights = {round_pair<DT>(p[0], p[1]), round_pair<DT>(p[2], p[3]), round_pair<DT>(p[4], p[5]), round_pair<DT>(p[6], p[7])};
         // values: words of eight codes, kJ codes to a token
@@ -459,7 +474,7 @@ template <int DIM> __device__ static inline void load_many(const char *block, ui
 }
 
 template <int DT, int DIM>
-__global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(AttendArgs a) {
+__global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_attend_many(AttendArgs a) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 16, kJ = DIM / 16, kD = DIM / 32;
     // Which part of a step goes before other wavefronts' work (4 prompts of 1024 rows, 4096 pairs each: heads of 64 scores 241 us, weights and outputs 262,
@@ -536,6 +551,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0;
     float base = -3.4028234663852886e38f, sum = 0;
+    bool far = false;                                     // far_out(base)
 
     // what is not held may be anything: its values are to be finite, its scores are masked
     auto blank = [&](int step, int id) {
@@ -631,18 +647,23 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : 2) void kv_attend_many(Attend
 #pragma unroll
             for (int e = 0; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
             top *= a.scale;
-            if (__any(top > base + WeightRange<DT>::kMost)) {
+            if (__any(top - base > WeightRange<DT>::kMost)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(base, top - WeightRange<DT>::kTop), keep = __builtin_amdgcn_exp2f(base - now);
+                const float now = raised<DT>(base, top), keep = __builtin_amdgcn_exp2f(base - now);
                 base = now;
+                far = far_out(base);
                 sum *= keep;
 #pragma unroll
                 for (int d = 0; d < kD; ++d) o[d] *= keep;
             }
+            const float factor = far ? 1.f : a.scale, less = far ? 0.f : base;
+            if (far)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) s[e / 16][e % 16] = in_twos(s[e / 16][e % 16], a.scale) - base;
             float part[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale, -base));
+                s[e / 16][e % 16] = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], factor, -less));
                 part[e % 4] += s[e / 16][e % 16];
             }
             sum += (part[0] + part[1]) + (part[2] + part[3]);

@@ -61,3 +61,23 @@ def test_scores_that_rise_or_fall(n, fresh, query, dtype):
     keys = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6])[level]
     values = torch.tensor([1., -2, 3, 4, -6, 1.5, 2, 0.5])[torch.arange(n) % 8]
     check(scene(dtype, n, fresh, keys, values, query), n, fresh)
+
+
+@pytest.mark.parametrize("n,fresh", [(700, 1), (5000, 1), (700, 40)])
+@pytest.mark.parametrize("exponent", [4, 8, 13, 30])
+@pytest.mark.parametrize("dtype", [nnv.F16, nnv.BF16])
+def test_scores_beyond_what_float32_counts_in_ones(n, fresh, exponent, dtype):
+    """One score is the largest by so much that nothing else weighs anything: the output is that token's value, however large the scores are."""
+    if dtype == nnv.F16 and exponent > 13:
+        exponent = 12                                        # (what float16 holds)
+    for query in (997.0, 1234.5, -3.0, 31000.0, 60000.0):
+        for order in (torch.arange(n), torch.arange(n).flip(0), (torch.arange(n) * 7919) % n):
+            levels = torch.tensor([0, .5, 1, 1.5, 2, 3, 4])[order * 7 // n]
+            at = int(order.argmax()) if fresh == 1 else int(order[: n - fresh].argmax())      # a token that all rows see
+            levels[at] = 6
+            if query < 0:
+                levels = -levels
+            values = torch.full((n,), -2.0)
+            values[at] = 3
+            s = scene(dtype, n, fresh, levels * 2.0 ** exponent, values, query)
+            assert (s.run() == 3).all()
