@@ -312,7 +312,7 @@ typedef struct {
 size_t nnv_linear_transformed_bytes(const nnv_linear_desc *desc);
 
 /* Bytes of scratch of nnv_linear_forward over m rows (0 if invalid, or for up to 16 rows): x in 8 bits with its scales, and where
- * the reduction is split, partial sums. */
+ * the reduction is split, partial sums.  More rows may need less, where they are split into fewer parts: a buffer for several sizes is to hold the most of them. */
 size_t nnv_linear_workspace_bytes(const nnv_linear_desc *desc, int m);
 
 /* Raw weights (n x k of desc.raw_dtype, rows of k) -> 8-bit codes in the order that the matrix instructions read, and scales.
@@ -402,7 +402,8 @@ int nnv_kv_read(const nnv_attention_desc *desc, int n, const int64_t *slots, con
  * Rows that see nothing (position below 0, no request, length 0) yield zeros; a query head that holds a NaN yields NaN.  Tokens whose table entry is no block
  * of the cache are not seen.  starts and lengths are clamped to what desc and n_rows allow; where starts do not begin at
  * 0 or do decrease, what rows that no request has yield is not defined.
- * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP.
+ * As with the products, more rows may need less of a workspace. */
 size_t nnv_kv_attention_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows);
 int nnv_kv_attention(const nnv_attention_desc *desc, int n_requests, int n_rows, const void *q, const int32_t *block_table, const int32_t *starts,
                      const int32_t *lengths, const int32_t *positions, const void *cache, void *out, void *workspace, size_t workspace_bytes,

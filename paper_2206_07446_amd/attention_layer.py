@@ -32,10 +32,9 @@ class AttentionLayer:
         bytes_ = lambda n: new(max(16, n), dtype=torch.uint8)  # noqa: E731
         self.qkv_tx, self.out_tx = (bytes_(nnv.nnv_linear_transformed_bytes(d)) for d in (self.qkv_desc, self.out_desc))
         self.cache = bytes_(nnv.nnv_kv_cache_bytes(self.desc))
-        # what a product of m rows needs of its scratch goes up and down with m: the larger of every size that a step can have
-        sizes = sorted({rows, requests, *range(1, min(rows, 512) + 1), *range(512, rows + 1, 64)})
-        need = max(max(nnv.nnv_linear_workspace_bytes(d, m) for d in (self.qkv_desc, self.out_desc)) for m in sizes)
-        need = max([need] + [nnv.nnv_kv_attention_workspace_bytes(self.desc, requests, m) for m in sizes])
+        # what a call over m rows needs of its scratch goes up and down with m, where the number of parts that it splits into changes: the most of every size
+        need = max(max(nnv.nnv_kv_attention_workspace_bytes(self.desc, requests, m), *(nnv.nnv_linear_workspace_bytes(d, m) for d in (self.qkv_desc, self.out_desc)))
+                   for m in range(1, rows + 1))
         self.workspace = bytes_(need)
         self.q_weight, self.k_weight = (torch.ones(head_dim, device=self.device) for _ in range(2))
         half = head_dim // 2

@@ -1,0 +1,23 @@
+"""The attention layer of attention_layer.py without a GPU: what it allocates holds every step that it may be asked for."""
+import pytest
+import torch
+
+import paper_2206_07446_amd as nnv
+from paper_2206_07446_amd.attention_layer import AttentionLayer
+
+# hidden, query heads, key heads, head size, requests, rows, tokens
+SHAPES = [(4096, 32, 8, 128, 1, 1024, 8192), (4096, 32, 8, 128, 2, 1024, 2048), (4096, 32, 8, 128, 4, 2048, 8192), (512, 8, 8, 64, 1, 1024, 16384),
+          (6144, 2, 1, 64, 3, 800, 300), (256, 4, 2, 64, 50, 20, 100), (512, 4, 1, 256, 7, 1500, 70000)]
+
+
+def make(hidden, q, kv, dim, requests, rows, tokens, **kw):
+    return AttentionLayer(hidden, q, kv, dim, requests, rows, tokens, device="cpu", **kw)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_the_workspace_holds_a_step_of_any_size(shape):
+    layer = make(*shape)
+    have, requests, rows = layer.workspace.numel(), *shape[4:6]
+    short = [m for m in range(1, rows + 1) if max(nnv.nnv_kv_attention_workspace_bytes(layer.desc, requests, m), nnv.nnv_linear_workspace_bytes(layer.qkv_desc, m),
+                                                  nnv.nnv_linear_workspace_bytes(layer.out_desc, m)) > have]
+    assert not short, f"{len(short)} sizes, {short[0]} to {short[-1]}"
