@@ -365,7 +365,8 @@ size_t nnv_kv_cache_bytes(const nnv_attention_desc *desc);
  *   free_left : one int32, what remains of the free list.  Apart from free_count, so that a call can be repeated
  * Requests are admitted whole and in order: one whose new tokens fit neither the block table nor n_rows is passed over,
  * and once the free list is too short for one that needs blocks, so it is for all after it that need any; lengths of those
- * are what they held.  A table entry that is no block of the cache gives slot -1.
+ * are what they held.  A table entry that is no block of the cache gives slot -1.  The rotation table is not looked at: where it has fewer positions than
+ * table_blocks x block_tokens, nnv_qk_norm_rope does not hold tokens that are counted here.
  * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, ALIGN, HIP. */
 int nnv_kv_plan(const nnv_attention_desc *desc, int n_requests, int n_rows, const int32_t *held, const int32_t *fresh,
                 const int32_t *free_blocks, const int32_t *free_count, int32_t *block_table, int32_t *starts, int32_t *lengths,

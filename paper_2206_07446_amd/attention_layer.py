@@ -16,14 +16,14 @@ DTYPES = {nnv.F16: torch.float16, nnv.BF16: torch.bfloat16}
 
 
 class AttentionLayer:
-    """Weights, cache, block table and buffers for up to `rows` rows a step and `requests` requests."""
+    """Weights, cache, block table and buffers for up to `rows` rows a step and `requests` requests of `tokens` tokens (whole blocks of them)."""
 
     def __init__(self, hidden, q_heads, kv_heads, head_dim, requests, rows, tokens, block_tokens=64, dtype=nnv.BF16, theta=10000.0, window=0, sinks=0,
                  device="cuda:0"):
         self.device, self.dtype, self.requests, self.rows, self.hidden = torch.device(device), DTYPES[dtype], requests, rows, hidden
         width = -(-tokens // block_tokens)
         self.desc = nnv.AttentionDesc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, block_tokens=block_tokens, blocks=requests * width,
-                                      table_blocks=width, rotary_dim=head_dim, rotary_interleaved=0, positions=tokens, window=window, sinks=sinks, dtype=dtype,
+                                      table_blocks=width, rotary_dim=head_dim, rotary_interleaved=0, positions=width * block_tokens, window=window, sinks=sinks, dtype=dtype,
                                       scale=head_dim ** -0.5, eps=1e-6)
         self.q_size, self.kv_size = q_heads * head_dim, kv_heads * head_dim
         self.qkv_desc = nnv.LinearDesc(n=self.q_size + 2 * self.kv_size, k=hidden, x_dtype=dtype, y_dtype=dtype, raw_dtype=nnv.F32)
@@ -38,7 +38,7 @@ class AttentionLayer:
         self.workspace = bytes_(need)
         self.q_weight, self.k_weight = (torch.ones(head_dim, device=self.device) for _ in range(2))
         half = head_dim // 2
-        angle = torch.arange(tokens, dtype=torch.float64)[:, None] * theta ** (-torch.arange(half, dtype=torch.float64) / half)
+        angle = torch.arange(width * block_tokens, dtype=torch.float64)[:, None] * theta ** (-torch.arange(half, dtype=torch.float64) / half)
         self.rope = torch.cat((angle.cos(), angle.sin()), 1).float().to(self.device)
         self.qkv, self.q, self.attended = new(rows, self.q_size + 2 * self.kv_size), new(rows, q_heads, head_dim), new(rows, q_heads, head_dim)
         ints = lambda n, dtype=torch.int32: torch.zeros(n, dtype=dtype, device=self.device)  # noqa: E731

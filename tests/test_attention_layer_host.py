@@ -21,3 +21,14 @@ def test_the_workspace_holds_a_step_of_any_size(shape):
     short = [m for m in range(1, rows + 1) if max(nnv.nnv_kv_attention_workspace_bytes(layer.desc, requests, m), nnv.nnv_linear_workspace_bytes(layer.qkv_desc, m),
                                                   nnv.nnv_linear_workspace_bytes(layer.out_desc, m)) > have]
     assert not short, f"{len(short)} sizes, {short[0]} to {short[-1]}"
+
+
+@pytest.mark.parametrize("tokens,block", [(100, 64), (120, 16), (128, 64), (1, 256)])
+def test_every_position_that_the_plan_admits_has_its_angles(tokens, block):
+    """A request is held in whole blocks, and so is what the plan lets in; a position behind the rotation table would be counted but not held."""
+    layer = make(256, 4, 2, 64, 3, 20, tokens, block_tokens=block)
+    capacity = layer.desc.table_blocks * layer.desc.block_tokens
+    assert capacity >= tokens and layer.desc.positions >= capacity and layer.rope.shape == (layer.desc.positions, 64)
+    last = torch.arange(32, dtype=torch.float64) / 32
+    want = (capacity - 1) * 10000.0 ** -last
+    assert torch.equal(layer.rope[capacity - 1], torch.cat((want.cos(), want.sin())).float())
