@@ -1,6 +1,6 @@
 """One attention layer of a language model as a serving program runs it, from request lengths to the layer's output
 rows: the cold start (weights to 8 bits), a step that takes the requests' prompts in, and steps of one token a request
-replayed from a HIP graph.  The layer keeps every buffer, so that a step is eight calls and no allocation.
+replayed from a HIP graph.  The layer keeps every buffer, so that a step is seven calls and no allocation.
 
 `python -m paper_2206_07446_amd.attention_layer --requests 64 --prompt 512 --steps 64` prints the time of each part.
 """
@@ -48,33 +48,52 @@ class AttentionLayer:
         self.free = torch.arange(requests * width, dtype=torch.int32, device=self.device)
         self.count = torch.tensor([requests * width], dtype=torch.int32, device=self.device)
 
+    def _check(self, rows, *tensors):
+        """The calls below take addresses: what their buffers do not hold is refused here."""
+        if not 0 <= rows <= self.rows:
+            raise ValueError(f"{rows} rows, the layer has buffers for 0 to {self.rows}")
+        for t in tensors:
+            if not (isinstance(t, torch.Tensor) and t.dtype == self.dtype and t.device == self.qkv.device and t.dim() == 2 and t.shape[0] >= rows
+                    and t.shape[1] == self.hidden and t.stride(1) == 1 and (rows <= 1 or t.stride(0) >= self.hidden) and t.data_ptr() % 16 == 0):
+                raise ValueError(f"expected {rows} rows or more of {self.hidden} {self.dtype} on {self.qkv.device}, each without gaps, the first 16-byte aligned")
+
     def transform_weights(self, w_qkv, w_out):
         """Raw float32 weights to the layouts that the products run from."""
+        for w, d in ((w_qkv, self.qkv_desc), (w_out, self.out_desc)):
+            if not (isinstance(w, torch.Tensor) and w.dtype == torch.float32 and w.device == self.qkv.device and w.shape == (d.n, d.k) and w.is_contiguous()):
+                raise ValueError(f"expected contiguous float32 weights of {d.n} x {d.k} on {self.qkv.device}")
         nnv.nnv_linear_transform_weights(self.qkv_desc, w_qkv, self.qkv_tx)
         nnv.nnv_linear_transform_weights(self.out_desc, w_out, self.out_tx)
 
     def plan(self, rows):
+        self._check(rows)
         nnv.nnv_kv_plan(self.desc, self.requests, rows, self.held, self.fresh, self.free, self.count, self.table, self.starts, self.lengths, self.positions,
                         self.slots, self.left)
 
     def project(self, x, rows):
+        self._check(rows, x)
         nnv.nnv_linear_forward(self.qkv_desc, rows, x, x.stride(0), self.qkv_tx, None, self.qkv, self.qkv.stride(0), self.workspace)
 
     def append(self, rows):
+        self._check(rows)
         stride = self.qkv.stride(0)
         q, k, v = self.qkv.split((self.q_size, self.kv_size, self.kv_size), 1)
         nnv.nnv_qk_norm_rope(self.desc, rows, q, stride, k, stride, v, stride, self.q_weight, self.k_weight, self.rope, self.positions, self.slots, self.q,
                              None, self.cache)
 
     def attend(self, rows):
+        self._check(rows)
         nnv.nnv_kv_attention(self.desc, self.requests, rows, self.q, self.table, self.starts, self.lengths, self.positions, self.cache, self.attended,
                              self.workspace)
 
     def finish(self, y, rows):
+        self._check(rows, y)
         nnv.nnv_linear_forward(self.out_desc, rows, self.attended, self.q_size, self.out_tx, None, y, y.stride(0), self.workspace)
 
     def step(self, x, y, rows):
-        """Rows of x (the new tokens of request 0, then of request 1, ..., as self.fresh counts them) -> rows of y; what is held grows by them."""
+        """Rows of x (the new tokens of request 0, then of request 1, ..., as self.fresh counts them) -> rows of y; what is held grows by them.  A step that its
+        buffers do not hold is refused before anything runs."""
+        self._check(rows, x, y)
         self.plan(rows)
         self.project(x, rows)
         self.append(rows)
