@@ -362,7 +362,9 @@ size_t nnv_kv_cache_bytes(const nnv_attention_desc *desc);
  *   starts : n_requests + 1 int32, row of each request's first new token, capped at n_rows
  *   lengths : n_requests int32, tokens of each request in the cache after the step
  *   positions, slots : n_rows int32 and int64, of each row; -1 for rows of no admitted request
- *   free_left : one int32, what remains of the free list.  Apart from free_count, so that a call can be repeated
+ *   free_left : one int32, what remains of the free list
+ * Outputs lie apart from the inputs and from each other, so that a call can be repeated (and workgroups read the inputs while others write): lengths in the place
+ * of held, free_left in that of free_count and other overlaps are refused.
  * Requests are admitted whole and in order: one whose new tokens fit neither the block table nor n_rows is passed over,
  * and once the free list is too short for one that needs blocks, so it is for all after it that need any; lengths of those
  * are what they held.  A table entry that is no block of the cache gives slot -1.  The rotation table is not looked at: where it has fewer positions than

@@ -51,6 +51,14 @@ int check_counts(int n_requests, int n_rows) {
     return n_requests < 0 || n_rows < 0 || n_requests > kMostRequests || n_rows > kMostRows ? NNV_E_ARG : NNV_OK;
 }
 
+// A buffer of a call, as bytes.
+struct Bytes {
+    uintptr_t at;
+    size_t count;
+    Bytes(const void *p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), count(p ? n : 0) {}
+    bool meets(const Bytes &o) const { return count && o.count && at < o.at + o.count && o.at < at + count; }
+};
+
 }  // namespace
 
 extern "C" {
@@ -98,7 +106,14 @@ int nnv_kv_plan(const nnv_attention_desc *desc, int n_requests, int n_rows, cons
     if (off4(held) || off4(fresh) || off4(free_blocks) || off4(free_count) || off4(block_table) || off4(starts) || off4(lengths) ||
         off4(positions) || off8(slots) || off4(free_left))
         return NNV_E_ALIGN;
-    if (free_left == free_count) return NNV_E_ARG;
+    // A workgroup reads all requests while others write: no output may lie in an input or in another output.  (How much of the free list is
+    // read is known on the device: here its first entry.)
+    const size_t n = n_requests, r = n_rows;
+    const Bytes buffers[] = {{held, 4 * n}, {fresh, 4 * n}, {free_blocks, 4}, {free_count, 4}, {block_table, 4 * n * desc->table_blocks}, {starts, 4 * (n + 1)},
+                             {lengths, 4 * n}, {positions, 4 * r}, {slots, 8 * r}, {free_left, 4}};
+    for (int out = 4; out < 10; ++out)
+        for (int other = 0; other < out; ++other)
+            if (buffers[out].meets(buffers[other])) return NNV_E_ARG;
     PlanArgs a{held, fresh, free_blocks, free_count, block_table, starts, lengths, positions, free_left, slots, n_requests, n_rows,
                log2_of(desc->block_tokens), desc->blocks, desc->table_blocks};
     return finish(launch_kv_plan(a, static_cast<hipStream_t>(hip_stream)));
