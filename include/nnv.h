@@ -324,7 +324,7 @@ int nnv_linear_transform_weights(const nnv_linear_desc *desc, const void *w_raw,
 /* y = x W^T + bias over m rows (0: nothing is done): x is rounded to 8 bits as above, products and sums are float32 on the
  * matrix cores, rounded once to desc.y_dtype.
  *   x : m rows of k elements, ldx >= k elements apart (any ldx; rows that are 16-byte aligned read faster)
- *   y : m rows of n elements, ldy >= n elements apart;  bias : n float32, or NULL
+ *   y : m rows of n elements, ldy >= n elements apart, none of them in a row of x (refused);  bias : n float32, or NULL
  *   workspace : >= nnv_linear_workspace_bytes(desc, m) bytes, whatever its contents
  * A row of x that holds a NaN or an infinity yields NaN in that row of y.
  * Errors: NULL, BAD_DESC, ARG, WORKSPACE, ALIGN, HIP. */

@@ -27,6 +27,30 @@ int check_linear(const nnv_linear_desc *d) {
     return NNV_OK;
 }
 
+// A buffer of a call, as bytes.
+struct Bytes {
+    uintptr_t at;
+    size_t count;
+    Bytes(const void *p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), count(p ? n : 0) {}
+    bool meets(const Bytes &o) const { return count && o.count && at < o.at + o.count && o.at < at + count; }
+};
+
+// Whether rows of two matrices meet, each given by its first row and the bytes from a row to the next (no fewer than a row has).  Columns of one buffer
+// may lie between each other, so where the whole of both overlaps, the rows are gone through in the order that they lie in.
+bool rows_meet(int m, Bytes a, int64_t a_stride, Bytes b, int64_t b_stride) {
+    typedef unsigned __int128 Wide;
+    const Wide a_end = a.at + (Wide)(m - 1) * a_stride + a.count, b_end = b.at + (Wide)(m - 1) * b_stride + b.count;
+    if (a.at >= b_end || b.at >= a_end) return false;
+    for (int i = 0, j = 0; i < m && j < m;) {
+        const Wide x = a.at + (Wide)i * a_stride, y = b.at + (Wide)j * b_stride;
+        if (x < y + b.count && y < x + a.count) return true;
+        if (x < y) ++i; else ++j;
+    }
+    return false;
+}
+
+int element_bytes(int dtype) { return dtype == NNV_F32 ? 4 : 2; }
+
 int log2_of(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
 
 int check_attention(const nnv_attention_desc *d) {
@@ -50,14 +74,6 @@ int check_attention(const nnv_attention_desc *d) {
 int check_counts(int n_requests, int n_rows) {
     return n_requests < 0 || n_rows < 0 || n_requests > kMostRequests || n_rows > kMostRows ? NNV_E_ARG : NNV_OK;
 }
-
-// A buffer of a call, as bytes.
-struct Bytes {
-    uintptr_t at;
-    size_t count;
-    Bytes(const void *p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), count(p ? n : 0) {}
-    bool meets(const Bytes &o) const { return count && o.count && at < o.at + o.count && o.at < at + count; }
-};
 
 }  // namespace
 
@@ -87,6 +103,9 @@ int nnv_linear_forward(const nnv_linear_desc *desc, int m, const void *x, int64_
     if (need && !workspace) return NNV_E_NULL;
     if (workspace_bytes < need) return NNV_E_WORKSPACE;
     if (off16(x) || off16(w_tx) || off16(y) || (need && off16(workspace)) || (bias && off4(bias))) return NNV_E_ALIGN;
+    const int xb = element_bytes(desc->x_dtype), yb = element_bytes(desc->y_dtype);
+    // (workgroups of other outputs still read x)
+    if (rows_meet(m, {x, (size_t)desc->k * xb}, m > 1 ? ldx * xb : 0, {y, (size_t)desc->n * yb}, m > 1 ? ldy * yb : 0)) return NNV_E_ARG;
     return finish(launch_linear(*desc, m, x, ldx, w_tx, bias, y, ldy, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
