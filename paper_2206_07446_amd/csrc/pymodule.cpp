@@ -40,7 +40,7 @@ template <typename T> bool as_struct(PyObject *o, PyObject *type, T *out) {
     }
     Py_buffer view;
     if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE)) return false;
-    const bool fits = view.len == (Py_ssize_t)sizeof(*out);
+    const bool fits = view.len >= (Py_ssize_t)sizeof(*out);      // a subclass may have fields behind the library's
     if (fits) memcpy(out, view.buf, sizeof(*out));
     else PyErr_Format(PyExc_TypeError, "%.100s of %zd bytes, %zd are wanted", Py_TYPE(o)->tp_name, view.len, (Py_ssize_t)sizeof(*out));
     PyBuffer_Release(&view);
