@@ -239,8 +239,9 @@ template <int DIM> __device__ static inline void load_step(const AttendArgs &a, 
 
 constexpr int kPartExtra = 4;      // floats of a partial result behind its values: base, sum, number of splits
 
-// Bound by memory where there is much to read (64 rows over up to 8192 tokens, 287 MB: 71 us, 4.0 TB/s, what a reduction reaches), and by the chain
-// of starts, table and codes where there is little (one row over 32768 tokens, 36 MB: 16 us).
+// Where there is much to read (64 rows over up to 8192 tokens, 287 MB: 71 us, 4.0 TB/s; a copy moves 5.2 TB/s here, half of it reads) vector instructions take 51 % of a
+// compute unit's busy time and its wavefronts wait for 46 % of theirs, so that neither is shown to bound alone; where there is little, the chain of starts, table
+// and codes does (one row over 32768 tokens, 36 MB: 16 us).
 // One (tile, key/value head, split): its wavefronts take steps in turn, each with a softmax of its own, and are joined in the LDS.  The next
 // step's loads are in flight while one is computed, the block numbers of the one after that too.
 //
@@ -429,7 +430,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
 // every 16 bytes a lane's part of an operand.  The four lanes' worth of a token's values that a lane has in hand go to rows that lie 8 apart;
 // the row is xor-ed with its sixteen, so that they meet different banks, and reading does so as well.
 // The conversions run beside the scores' products, the exponentials beside the outputs'.  4 prompts of 1024 rows over 876 to 6000 tokens, 32 heads of
-// 128 and 8 of keys: 203-212 us, 0.93-0.97 PFLOP/s of what the rows see; vector instructions take 60 % of a compute unit's busy time, matrix ones 47 %,
+// 128 and 8 of keys: 203-213 us, 0.93-0.97 PFLOP/s of what the rows see; vector instructions take 60 % of a compute unit's busy time, matrix ones 47 %,
 // and two workgroups that do not wait for one another are what lets them overlap (one of eight wavefronts for 256 pairs, with half the
 // conversions: 327 us).
 constexpr int kManyStep = 64, kManyRows = 128;
@@ -772,9 +773,11 @@ static bool attend_many(const nnv_attention_desc &d, int requests, int rows) { r
 
 // Splits of a tile's tokens, from what the host knows: 1024 workgroups where there are that few (four to a compute unit), or 512 of up to 8 tiles of rows,
 // which end together or have the chip to themselves (with 1024: 4 requests of up to 16000 tokens and 8 heads 22.5 us, 18.5 so; 8 of up to 12000 and 4 heads of 256
-// 28.7, 23.1 so; but 16 requests of 8 rows, up to 4096 tokens and 8 heads 32 us with 1024, 36 with 512); of at least 512 tokens (with 256 one request of 32768 tokens and
-// 8 heads takes 26 us, more partial results to join, against 20), at most 2048 of them, or 8192 where there are tiles enough, within 256 MB of partial results.
+// 28.7, 23.1 so; but 16 requests of 8 rows, up to 4096 tokens and 8 heads 32 us with 1024, 36 with 512); of at least 512 tokens of as long a request as the
+// table has room for (with 256 one request of 32768 tokens and 8 heads takes 26 us, more partial results to join, against 20; a shorter request beside it is cut into as
+// many, down to a round of the wavefronts each), at most 2048 of them, or 8192 where there are tiles enough, within 256 MB of partial results.
 static int attend_splits(const nnv_attention_desc &d, int requests, int rows) {
+    // (One number for both kernels: running requests beside a prompt get the prompt's.)
     const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens;
     const int64_t reach = d.window && (int64_t)d.window + d.sinks < capacity ? (int64_t)d.window + d.sinks : capacity;
     const bool many = attend_many(d, requests, rows);
