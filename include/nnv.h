@@ -416,6 +416,81 @@ int nnv_kv_attention(const nnv_attention_desc *desc, int n_requests, int n_rows,
                      const int32_t *lengths, const int32_t *positions, const void *cache, void *out, void *workspace, size_t workspace_bytes,
                      void *hip_stream);
 
+/* ---- attention over selected blocks: of a long request, each row and key head sees only some of the cache's blocks, those whose keys could give its query
+ * heads the largest scores.  What a block's keys could give is read from their bounds, which a step updates for the blocks that it wrote.  The calls take
+ * descriptors without a window (UNSUPPORTED): the selection takes its place. */
+
+/* Bytes of the bounds (0 if the descriptor is invalid): blocks x kv_heads x 2 x head_dim bfloat16, the largest values of a block's keys, then the smallest. */
+size_t nnv_kv_bounds_bytes(const nnv_attention_desc *desc);
+
+/* Bounds of the blocks that hold a step's new tokens, from the first of them to the last, over all tokens that are held there (bfloat16 has every value of the cache).
+ *   block_table, starts, lengths : as nnv_kv_plan writes them; request i has starts[i + 1] - starts[i] new tokens, the last of lengths[i]
+ *   bounds : of the other blocks are left as they are
+ * A block takes new tokens of one request only.  Table entries that are no block of the cache are passed over.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, ALIGN, HIP. */
+int nnv_kv_bounds(const nnv_attention_desc *desc, int n_requests, int n_rows, const int32_t *block_table, const int32_t *starts, const int32_t *lengths,
+                  const void *cache, void *bounds, void *hip_stream);
+
+/* The blocks that rows select, by place in their request (token / block_tokens): of those that a row sees (the blocks of tokens j <= p, j < lengths[i])
+ * the first n_first and the last n_last, and of the others those of the largest scores, `keep` in all or as many as there are.  The score is the
+ * largest, over the query heads that read key head h, of the sum over d of max(q[d] hi[d], q[d] lo[d]) (with -q in the place of q where desc.scale is negative), in float64;
+ * equal ones go to the lower block, sums that are no number count as -infinity.  Products of a query's 8 or 11 bits with a bound's 2 are exact there, and
+ * so are sums whose terms span fewer than 2^40: then the selection depends on no order.
+ *   selected : n_rows x kv_heads x keep int32, ascending, -1 behind the last (and in rows that see nothing)
+ *   workspace : >= nnv_kv_select_workspace_bytes(desc, n_requests, n_rows) bytes, whatever its contents
+ * 1 <= keep <= 2^20, n_first, n_last >= 0, n_first + n_last <= keep; at most 32768 table_blocks (UNSUPPORTED).  Blocks whose table entry is none of the cache are not selected.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
+size_t nnv_kv_select_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows);
+int nnv_kv_select(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep, int n_first, int n_last, const void *q, const int32_t *block_table,
+                  const int32_t *starts, const int32_t *lengths, const int32_t *positions, const void *bounds, int32_t *selected, void *workspace,
+                  size_t workspace_bytes, void *hip_stream);
+
+/* Attention as nnv_kv_attention, of each row and key head over the tokens of its selected blocks only.
+ *   selected : n_rows x kv_heads x keep int32 (1 <= keep <= 2^20), as nnv_kv_select writes them or any other: in any order; what is below 0 or behind the row's position is passed
+ *              over, and a block that is given twice counts twice
+ *   workspace : >= nnv_kv_attention_blocks_workspace_bytes(desc, n_requests, n_rows, keep) bytes, whatever its contents; out lies apart from the inputs
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
+size_t nnv_kv_attention_blocks_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep);
+int nnv_kv_attention_blocks(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep, const void *q, const int32_t *block_table,
+                            const int32_t *starts, const int32_t *lengths, const int32_t *positions, const int32_t *selected, const void *cache, void *out,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Attention as nnv_kv_attention, of requests that begin with the same tokens: these are read once for all of a group.
+ *   groups : n_groups + 1 int32, ascending: group g is requests groups[g] to groups[g + 1] - 1; requests of no group have nothing in common
+ *   shared : n_groups int32, tokens that the group has in common: those of its first request's table, as many as that holds (lengths[groups[g]]) at most.  A
+ *            row of request i sees of these the tokens j <= p, and behind them those of its own table, j < lengths[i]; positions, window and sinks count from the request's
+ *            first token as ever.  Other requests' table entries of blocks that lie whole within the common tokens are not looked at
+ *   workspace : >= nnv_kv_attention_shared_workspace_bytes(desc, n_requests, n_rows, n_groups) bytes, whatever its contents; out lies apart from the inputs
+ * Where groups are not ascending, what their rows yield is not defined.
+ * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
+size_t nnv_kv_attention_shared_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups);
+int nnv_kv_attention_shared(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups, const void *q, const int32_t *block_table,
+                            const int32_t *starts, const int32_t *lengths, const int32_t *positions, const int32_t *groups, const int32_t *shared,
+                            const void *cache, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The step between two blocks of a model: a block's output onto the residual stream, and the next block's norm of that. */
+typedef struct {
+    int32_t n;                         /* values of a row, at most 32768 */
+    int32_t x_dtype, y_dtype, h_dtype; /* nnv_dtype of the stream, of the block's output and the gates, of the norm */
+    float scale;                       /* factor of what is added */
+    float eps;                         /* of the norms */
+} nnv_residual_desc;
+
+/* r = x + scale * gate * norm(y), x_out = r, h = norm(r) over m rows (0: nothing is done), with norm(v) = v / sqrt(mean(v^2) + eps) * weight.  Values are
+ * float32 from the loads to the stores, which round once: h is of r before it is rounded to x_out.
+ *   x, x_out : rows of n elements, ldx, ldo elements apart; x_out may be x itself (with the same distance), so that the stream is updated in place
+ *   y    : the block's output, ldy apart.  NULL: r is x, and post, gate, index and x_out are not looked at
+ *   post : n float32, weight of the norm of y; NULL: y as it is
+ *   gate : `gates` rows of n elements of desc.y_dtype, ldg apart; NULL: none.  index NULL: row i has gate i (gates >= m) or all rows the same (gates 1);
+ *          otherwise m int32, and a row of an index that is none of the gates has r = x
+ *   pre  : n float32, weight of the norm of r; NULL: h is not looked at
+ * Distances are at least n (any; of a single row they are not looked at).  Outputs lie apart from every input and from each other but for x_out in the place of x
+ * (refused).  A row of zeros with eps 0 has a norm of zeros; a NaN in a row makes its norms NaN.
+ * Errors: NULL, BAD_DESC, ARG, ALIGN, HIP. */
+int nnv_residual_norm(const nnv_residual_desc *desc, int m, const void *x, int64_t ldx, const void *y, int64_t ldy, const float *post, int gates,
+                      const void *gate, int64_t ldg, const int32_t *index, const float *pre, void *x_out, int64_t ldo, void *h, int64_t ldh,
+                      void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -143,3 +143,48 @@ def attention(q, k, v, positions, scale, window=0, sinks=0, seen=None):
 def score_bound(dim, most):
     """How far a float32 score may be from its value, in units of the exponent: products and sums of dim terms, the two scalings."""
     return (dim + 8) * 2.0 ** -23 * most
+
+
+def bounds(k):
+    """k (tokens, heads, dim) as the cache holds them -> (heads, 2, dim): the largest, then the smallest."""
+    return np.stack((k.max(0), k.min(0)), 1)
+
+
+def block_scores(q, block_bounds, negative=False):
+    """q (heads, dim) over bounds (blocks, kv heads, 2, dim) -> (kv heads, blocks): what a key within the bounds could give, the largest of a group's heads; a sum
+    that is no number counts as -infinity."""
+    blocks, kv, _, dim = block_bounds.shape
+    out = np.full((kv, blocks), -np.inf)
+    with np.errstate(invalid="ignore"):
+        for h in range(q.shape[0]):
+            g = h // (q.shape[0] // kv)
+            a, b = q[h] * block_bounds[:, g, 0], q[h] * block_bounds[:, g, 1]
+            s = (-np.fmin(a, b) if negative else np.fmax(a, b)).sum(-1)
+            out[g] = np.maximum(out[g], np.where(np.isnan(s), -np.inf, s))
+    return out
+
+
+def select(scores, visible, keep, first, last, there):
+    """scores (kv heads, blocks), blocks that a row sees -> (kv heads, keep), -1 behind the last; there: blocks that the cache has."""
+    out = np.full((scores.shape[0], keep), -1, np.int64)
+    for g in range(scores.shape[0]):
+        always = [b for b in range(visible) if there[b] and (b < first or b >= visible - last)]
+        others = sorted((b for b in range(visible) if there[b] and b not in always), key=lambda b: (-scores[g, b], b))
+        chosen = sorted(always + others[: keep - len(always)])
+        out[g, : len(chosen)] = chosen
+    return out
+
+
+def residual_norm(x, y, post, gate, scale, eps, pre):
+    """-> (r, norm of r, sum of the magnitudes of r's terms); y, post, gate (a row each) and pre may be None."""
+    def norm(v, weight):
+        mean = (v * v).mean(-1, keepdims=True) + eps
+        return np.where(mean == 0, 0.0, v / np.sqrt(np.where(mean == 0, 1, mean))) * weight
+
+    add = np.zeros_like(x) if y is None else y
+    if post is not None and y is not None:
+        add = norm(add, post)
+    if gate is not None and y is not None:
+        add = add * gate
+    r = x + scale * add
+    return r, None if pre is None else norm(r, pre), np.abs(x) + np.abs(scale * add)

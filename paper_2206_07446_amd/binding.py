@@ -27,7 +27,9 @@ EXPORTS = ("nnv_layout_version", "nnv_status_string", "nnv_last_hip_error", "nnv
            "nnv_conv_forward_grouped_workspace_bytes", "nnv_time_layer", "nnv_cold_stack", "nnv_cache_write",
            "nnv_cache_read", "nnv_linear_transformed_bytes", "nnv_linear_workspace_bytes", "nnv_linear_transform_weights",
            "nnv_linear_forward", "nnv_kv_cache_bytes", "nnv_kv_plan", "nnv_qk_norm_rope", "nnv_kv_read",
-           "nnv_kv_attention_workspace_bytes", "nnv_kv_attention")
+           "nnv_kv_attention_workspace_bytes", "nnv_kv_attention", "nnv_kv_bounds_bytes", "nnv_kv_bounds",
+           "nnv_kv_select_workspace_bytes", "nnv_kv_select", "nnv_kv_attention_blocks_workspace_bytes", "nnv_kv_attention_blocks",
+           "nnv_kv_attention_shared_workspace_bytes", "nnv_kv_attention_shared", "nnv_residual_norm")
 
 
 class NnvError(RuntimeError):
@@ -64,6 +66,11 @@ class AttentionDesc(Structure):
     """An attention layer over a cache of blocks held in 4 bits (nnv_attention_desc)."""
     _fields_ = [(n, c_int32) for n in ("q_heads", "kv_heads", "head_dim", "block_tokens", "blocks", "table_blocks", "rotary_dim", "rotary_interleaved",
                                        "positions", "window", "sinks", "dtype")] + [("scale", c_float), ("eps", c_float)]
+
+
+class ResidualDesc(Structure):
+    """The step from a block's output to the next block's norm (nnv_residual_desc)."""
+    _fields_ = [(n, c_int32) for n in ("n", "x_dtype", "y_dtype", "h_dtype")] + [(n, c_float) for n in ("scale", "eps")]
 
 
 _lib = None
@@ -138,6 +145,21 @@ def load():
     lib.nnv_kv_attention_workspace_bytes.argtypes = [POINTER(AttentionDesc), c_int, c_int]
     lib.nnv_kv_attention.restype = c_int
     lib.nnv_kv_attention.argtypes = [POINTER(AttentionDesc), c_int, c_int] + [c_void_p] * 8 + [c_size_t, c_void_p]
+    lib.nnv_kv_bounds_bytes.restype = c_size_t
+    lib.nnv_kv_bounds_bytes.argtypes = [POINTER(AttentionDesc)]
+    lib.nnv_kv_bounds.restype = c_int
+    lib.nnv_kv_bounds.argtypes = [POINTER(AttentionDesc), c_int, c_int] + [c_void_p] * 6
+    lib.nnv_kv_select_workspace_bytes.restype = c_size_t
+    lib.nnv_kv_select_workspace_bytes.argtypes = [POINTER(AttentionDesc), c_int, c_int]
+    lib.nnv_kv_select.restype = c_int
+    lib.nnv_kv_select.argtypes = [POINTER(AttentionDesc)] + [c_int] * 5 + [c_void_p] * 8 + [c_size_t, c_void_p]
+    for name, arrays in (("blocks", 9), ("shared", 10)):
+        size, call = (getattr(lib, f"nnv_kv_attention_{name}{end}") for end in ("_workspace_bytes", ""))
+        size.restype, size.argtypes = c_size_t, [POINTER(AttentionDesc), c_int, c_int, c_int]
+        call.restype, call.argtypes = c_int, [POINTER(AttentionDesc), c_int, c_int, c_int] + [c_void_p] * arrays + [c_size_t, c_void_p]
+    lib.nnv_residual_norm.restype = c_int
+    lib.nnv_residual_norm.argtypes = [POINTER(ResidualDesc), c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p, c_int64, c_void_p,
+                                      c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
     _native = _load_module(torch)
     _lib = lib
     return lib
@@ -156,7 +178,7 @@ def _load_module(torch):
         return _CtypesCalls
     native.setup(ConvDesc, _fail, lambda: torch.cuda.current_stream().cuda_stream, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
                  getattr(torch._C, "_cuda_getCurrentRawStream", None))
-    native.setup_serving(LinearDesc, AttentionDesc)
+    native.setup_serving(LinearDesc, AttentionDesc, ResidualDesc)
     return native
 
 
@@ -298,6 +320,35 @@ class _CtypesCalls:
                                        _ptr(positions), _ptr(cache), _ptr(out), _ptr(workspace), _size(workspace, workspace_bytes),
                                        _stream(stream)), "nnv_kv_attention")
 
+    @staticmethod
+    def kv_bounds(desc, n_requests, n_rows, block_table, starts, lengths, cache, bounds, stream):
+        _check(load().nnv_kv_bounds(byref(desc), _int(n_requests), _int(n_rows), _ptr(block_table), _ptr(starts), _ptr(lengths), _ptr(cache), _ptr(bounds),
+                                    _stream(stream)), "nnv_kv_bounds")
+
+    @staticmethod
+    def kv_select(desc, n_requests, n_rows, keep, n_first, n_last, q, block_table, starts, lengths, positions, bounds, selected, workspace, workspace_bytes, stream):
+        _check(load().nnv_kv_select(byref(desc), _int(n_requests), _int(n_rows), _int(keep), _int(n_first), _int(n_last), _ptr(q), _ptr(block_table),
+                                    _ptr(starts), _ptr(lengths), _ptr(positions), _ptr(bounds), _ptr(selected), _ptr(workspace),
+                                    _size(workspace, workspace_bytes), _stream(stream)), "nnv_kv_select")
+
+    @staticmethod
+    def kv_attention_blocks(desc, n_requests, n_rows, keep, q, block_table, starts, lengths, positions, selected, cache, out, workspace, workspace_bytes, stream):
+        _check(load().nnv_kv_attention_blocks(byref(desc), _int(n_requests), _int(n_rows), _int(keep), _ptr(q), _ptr(block_table), _ptr(starts), _ptr(lengths),
+                                              _ptr(positions), _ptr(selected), _ptr(cache), _ptr(out), _ptr(workspace), _size(workspace, workspace_bytes),
+                                              _stream(stream)), "nnv_kv_attention_blocks")
+
+    @staticmethod
+    def kv_attention_shared(desc, n_requests, n_rows, n_groups, q, block_table, starts, lengths, positions, groups, shared, cache, out, workspace,
+                            workspace_bytes, stream):
+        _check(load().nnv_kv_attention_shared(byref(desc), _int(n_requests), _int(n_rows), _int(n_groups), _ptr(q), _ptr(block_table), _ptr(starts),
+                                              _ptr(lengths), _ptr(positions), _ptr(groups), _ptr(shared), _ptr(cache), _ptr(out), _ptr(workspace),
+                                              _size(workspace, workspace_bytes), _stream(stream)), "nnv_kv_attention_shared")
+
+    @staticmethod
+    def residual_norm(desc, m, x, ldx, y, ldy, post, gates, gate, ldg, index, pre, x_out, ldo, h, ldh, stream):
+        _check(load().nnv_residual_norm(byref(desc), _int(m), _ptr(x), ldx, _ptr(y), ldy, _ptr(post), _int(gates), _ptr(gate), ldg, _ptr(index), _ptr(pre),
+                                        _ptr(x_out), ldo, _ptr(h), ldh, _stream(stream)), "nnv_residual_norm")
+
 
 def nnv_layout_version() -> int:
     return load().nnv_layout_version()
@@ -431,3 +482,46 @@ def nnv_kv_attention(desc: AttentionDesc, n_requests: int, n_rows: int, q, block
                      workspace_bytes=None, stream=None) -> None:
     (_native or _calls()).kv_attention(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes,
                                        stream)
+
+
+def nnv_kv_bounds_bytes(desc: AttentionDesc) -> int:
+    return int(load().nnv_kv_bounds_bytes(byref(desc)))
+
+
+def nnv_kv_bounds(desc: AttentionDesc, n_requests: int, n_rows: int, block_table, starts, lengths, cache, bounds, stream=None) -> None:
+    (_native or _calls()).kv_bounds(desc, n_requests, n_rows, block_table, starts, lengths, cache, bounds, stream)
+
+
+def nnv_kv_select_workspace_bytes(desc: AttentionDesc, n_requests: int, n_rows: int) -> int:
+    return int(load().nnv_kv_select_workspace_bytes(byref(desc), _int(n_requests), _int(n_rows)))
+
+
+def nnv_kv_select(desc: AttentionDesc, n_requests: int, n_rows: int, keep: int, n_first: int, n_last: int, q, block_table, starts, lengths, positions,
+                  bounds, selected, workspace, workspace_bytes=None, stream=None) -> None:
+    (_native or _calls()).kv_select(desc, n_requests, n_rows, keep, n_first, n_last, q, block_table, starts, lengths, positions, bounds, selected, workspace,
+                                    workspace_bytes, stream)
+
+
+def nnv_kv_attention_blocks_workspace_bytes(desc: AttentionDesc, n_requests: int, n_rows: int, keep: int) -> int:
+    return int(load().nnv_kv_attention_blocks_workspace_bytes(byref(desc), _int(n_requests), _int(n_rows), _int(keep)))
+
+
+def nnv_kv_attention_blocks(desc: AttentionDesc, n_requests: int, n_rows: int, keep: int, q, block_table, starts, lengths, positions, selected, cache, out,
+                            workspace, workspace_bytes=None, stream=None) -> None:
+    (_native or _calls()).kv_attention_blocks(desc, n_requests, n_rows, keep, q, block_table, starts, lengths, positions, selected, cache, out, workspace,
+                                              workspace_bytes, stream)
+
+
+def nnv_kv_attention_shared_workspace_bytes(desc: AttentionDesc, n_requests: int, n_rows: int, n_groups: int) -> int:
+    return int(load().nnv_kv_attention_shared_workspace_bytes(byref(desc), _int(n_requests), _int(n_rows), _int(n_groups)))
+
+
+def nnv_kv_attention_shared(desc: AttentionDesc, n_requests: int, n_rows: int, n_groups: int, q, block_table, starts, lengths, positions, groups, shared,
+                            cache, out, workspace, workspace_bytes=None, stream=None) -> None:
+    (_native or _calls()).kv_attention_shared(desc, n_requests, n_rows, n_groups, q, block_table, starts, lengths, positions, groups, shared, cache, out,
+                                              workspace, workspace_bytes, stream)
+
+
+def nnv_residual_norm(desc: ResidualDesc, m: int, x, ldx: int, y, ldy: int, post, gates: int, gate, ldg: int, index, pre, x_out, ldo: int, h, ldh: int,
+                      stream=None) -> None:
+    (_native or _calls()).residual_norm(desc, m, x, ldx, y, ldy, post, gates, gate, ldg, index, pre, x_out, ldo, h, ldh, stream)

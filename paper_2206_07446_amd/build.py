@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libnnv.so")
 # the suffix names the interpreter and its ABI: another Python does not load what this one built
 MODULE = os.path.join(HERE, "_nnvpy" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ("api.cpp", "cache.cpp", "transform.hip", "direct.hip", "gemm.hip", "winograd.hip",
-           "serving.cpp", "linear.hip", "kv.hip", "attention.hip")
+           "serving.cpp", "linear.hip", "kv.hip", "attention.hip", "select.hip", "norm.hip")
 # packed-fp32 VALU instructions are switched off for every device translation unit
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -86,6 +86,10 @@ __device__ static inline int wave_max(int v) {
 // x / group for x below 2 x 1024: rounded up 2^21 / group times x is off by less than x * group <= 2^21 parts of 2^21.
 __device__ static inline int by_group(const AttendArgs &a, int x) { return (int)((uint32_t)x * a.group_inverse >> 21); }
 
+// Which tokens the rows of a launch see: all of their request's; of a group of requests those that they have in common; of a request those behind the ones that it
+// has in common with others; or those of the blocks that a row and key head's list names.
+enum Seen { kAll, kPrefix, kOwn, kListed };
+
 // A tile of a request: R consecutive pairs of a row and a query head of the group.
 struct Tile {
     int request, row0, pair0, pairs;     // first row of the request, first pair of the tile, pairs in it
@@ -94,6 +98,43 @@ struct Tile {
 
 // Whatever starts and lengths hold, a tile stays within a.rows rows.
 __device__ static inline int clamped_start(const AttendArgs &a, int v) { return min(max(v, 0), a.rows); }
+
+__device__ static inline int capacity_of(const AttendArgs &a) { return (int)min((int64_t)a.width << a.block_log, (int64_t)0x7fffffff); }
+
+// Whatever groups and shared hold: the first request of group i (or of none), and how many tokens the group has in common.
+__device__ static inline int leader_of(const AttendArgs &a, int i) { return min(max(a.groups[i], 0), a.requests); }
+__device__ static inline int prefix_of(const AttendArgs &a, int i) {
+    const int leader = leader_of(a, i), held = leader < a.requests ? a.lengths[leader] : 0;
+    return max(min(min(a.shared[i], held), capacity_of(a)), 0);
+}
+// Of a request; 0 where no group has it.
+__device__ static inline int request_prefix(const AttendArgs &a, int request) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, span = a.n_groups;
+    while (span > 0) {
+        const int each = (span + 63) / 64, i = lo + lane * each;
+        const bool mine = lane * each < span;
+        const bool before = mine && leader_of(a, mine ? i : lo) <= request;
+        const int held = before && each == 1 && request < leader_of(a, i + 1) ? prefix_of(a, i) : 0;
+        const int n = __builtin_popcountll(__ballot(before));
+        if (n == 0) return 0;
+        if (each == 1) return __builtin_amdgcn_readlane(held, n - 1);
+        lo = uniform(lo + (n - 1) * each);
+        span = uniform(min(each, span - (n - 1) * each));
+    }
+    return 0;
+}
+
+// What a launch's rows are divided by: requests, or groups of them.
+template <int SEEN> __device__ static inline int units_of(const AttendArgs &a) { return SEEN == kPrefix ? a.n_groups : a.requests; }
+template <int SEEN> __device__ static inline int start_of(const AttendArgs &a, int i) {
+    if constexpr (SEEN == kPrefix) return clamped_start(a, a.starts[leader_of(a, i)]);
+    return clamped_start(a, a.starts[i]);
+}
+template <int SEEN> __device__ static inline int length_of(const AttendArgs &a, int i) {
+    if constexpr (SEEN == kPrefix) return prefix_of(a, i);
+    return a.lengths[i];
+}
 
 // Tile `local` of a request, from what starts and lengths hold for it.
 template <int R> __device__ static inline Tile tile_of(const AttendArgs &a, int request, int start, int end, int length, int64_t local) {
@@ -111,14 +152,14 @@ template <int R> __device__ static inline Tile tile_of(const AttendArgs &a, int 
 // Finds tile u.  Tiles of request i start at floor(starts[i] * group / R) + i: enough for its pairs, with gaps (pairs = 0); request `requests`
 // stands for the rows that belong to none.  Every wavefront does so by itself: 64 starts at a time are compared with u, and in the last round,
 // the only one of up to 63 requests, come with the starts after them and the lengths, so that a chain of loads is one link long.
-template <int R> __device__ static inline Tile find_tile(const AttendArgs &a, int u) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, span = a.requests + 1;
+template <int R, int SEEN> __device__ static inline Tile find_tile(const AttendArgs &a, int u) {
+    const int lane = threadIdx.x & 63, units = units_of<SEEN>(a);
+    int lo = 0, span = units + 1;
     for (;;) {
         const int each = (span + 63) / 64, i = lo + lane * each;
-        const bool mine = lane * each < span, request = mine && i < a.requests;
-        const int start = mine ? clamped_start(a, a.starts[i]) : a.rows;
-        const int end = each == 1 && request ? clamped_start(a, a.starts[i + 1]) : a.rows, length = each == 1 && request ? a.lengths[i] : 0;
+        const bool mine = lane * each < span, request = mine && i < units;
+        const int start = mine ? start_of<SEEN>(a, i) : a.rows;
+        const int end = each == 1 && request ? start_of<SEEN>(a, i + 1) : a.rows, length = each == 1 && request ? length_of<SEEN>(a, i) : 0;
         const int n = max(__builtin_popcountll(__ballot(mine && (int64_t)start * a.group / R + i <= u)), 1);
         lo = uniform(lo + (n - 1) * each);
         span = uniform(min(each, span - (n - 1) * each));
@@ -153,17 +194,43 @@ template <int R> __device__ static inline Tile find_longest(const AttendArgs &a,
                       __builtin_amdgcn_readlane(before + tiles, at) - 1 - u);
 }
 
-// Which steps of S tokens rows at positions `lowest` (of those that see anything) to `highest` see: [0, sinks) and [first, first + count - sinks).
+// A row's tile of R query heads of a group, and the request that it belongs to.
+template <int R> __device__ static inline Tile find_row(const AttendArgs &a, int row, int first_head) {
+    const int lane = threadIdx.x & 63;
+    Tile t{};
+    int lo = 0, span = a.requests;
+    t.request = a.requests;
+    while (span > 0) {
+        const int each = (span + 63) / 64, i = lo + lane * each;
+        const bool mine = lane * each < span;
+        const int n = __builtin_popcountll(__ballot(mine && clamped_start(a, a.starts[mine ? i : lo]) <= row));
+        if (n == 0) break;
+        lo = uniform(lo + (n - 1) * each);
+        span = uniform(min(each, span - (n - 1) * each));
+        if (each > 1) continue;
+        if (row < clamped_start(a, a.starts[lo + 1])) t.request = lo;
+        break;
+    }
+    t.row0 = row;
+    t.pair0 = first_head;
+    t.pairs = min(R, a.group - first_head);
+    t.length = t.request < a.requests ? min(max(a.lengths[t.request], 0), capacity_of(a)) : 0;
+    return t;
+}
+
+// Which steps of S tokens rows at positions `lowest` (of those that see anything) to `highest` see of the tokens from `from` on: [low, low + sinks) and
+// [first, first + count - sinks).
 struct Steps {
-    int count, sinks, first;
-    __device__ int at(int i) const { return i < sinks ? i : first + i - sinks; }
+    int count, sinks, first, low;
+    __device__ int at(int i) const { return i < sinks ? low + i : first + i - sinks; }
 };
-template <int S> __device__ static inline Steps steps_of(const AttendArgs &a, int lowest, int highest, int length) {
+template <int S> __device__ static inline Steps steps_of(const AttendArgs &a, int lowest, int highest, int length, int from) {
     const int end_token = min(highest, length - 1) + 1, end = (end_token + S - 1) / S;
     Steps s;
-    s.sinks = a.window ? min((a.sinks + S - 1) / S, end) : 0;
-    s.first = max(a.window ? max(lowest - a.window + 1, 0) / S : 0, s.sinks);
-    s.count = end_token > 0 ? s.sinks + max(0, end - s.first) : 0;
+    s.low = from / S;
+    s.sinks = a.window ? max(min((a.sinks + S - 1) / S, end) - s.low, 0) : 0;
+    s.first = max(a.window ? max(lowest - a.window + 1, 0) / S : 0, s.low + s.sinks);
+    s.count = end_token > from ? s.sinks + max(0, end - s.first) : 0;
     return s;
 }
 
@@ -206,10 +273,10 @@ __device__ static inline TableRow table_row(const AttendArgs &a, int request) {
     return reinterpret_cast<TableRow>(reinterpret_cast<uintptr_t>(a.table + (int64_t)request * a.width));
 }
 
-// Blocks of the two sixteens of a step (a sixteen lies in one block); -1: none, or behind the request's tokens.
-struct StepBlocks { int id[2]; };
+// Blocks of the two sixteens of a step (a sixteen lies in one block); -1: none, or behind the request's tokens.  token: the first of each, where a list says which.
+struct StepBlocks { int id[2], token[2]; };
 __device__ static inline StepBlocks blocks_of(const AttendArgs &a, TableRow table, int step, int length) {
-    StepBlocks s;
+    StepBlocks s = {};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int token0 = step * kStep + i * 16;
@@ -237,7 +304,8 @@ template <int DIM> __device__ static inline void load_step(const AttendArgs &a, 
     }
 }
 
-constexpr int kPartExtra = 4;      // floats of a partial result behind its values: base, sum, number of splits
+constexpr int kPartExtra = 4;      // floats of a partial result behind its values: base, sum, number of splits, whether there are any of a prefix
+constexpr int kFewest = 512;       // tokens of a split at least, where the host knows no bound near their number
 
 // Where there is much to read (64 rows over up to 8192 tokens, 287 MB: 71 us, 4.0 TB/s; a copy moves 5.2 TB/s here, half of it reads) vector instructions take 51 % of a
 // compute unit's busy time and its wavefronts wait for 46 % of theirs, so that neither is shown to bound alone; where there is little, the chain of starts, table
@@ -248,7 +316,7 @@ constexpr int kPartExtra = 4;      // floats of a partial result behind its valu
 // A column's scores are taken relative to a base that all its lanes share.  It need not be the maximum: it is raised,
 // and what was summed is scaled down, only when a weight of the wavefront would pass the most of WeightRange, which past the
 // first steps is hardly ever.
-template <int DT, int DIM>
+template <int DT, int DIM, int SEEN>
 __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_attend(AttendArgs a) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 32, kJ = DIM / 16;          // instructions of a score, of an output
@@ -258,9 +326,17 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
     const int u = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles, head = rest % a.kv_heads, split = rest / a.kv_heads;
     // beside kv_attend_many, requests of fewer than 32 pairs: two tiles each
     static_assert(kManyPairs <= 2 * kTileRows, "two tiles hold them");
-    const Tile t = a.many ? tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2)
-                          : find_tile<kTileRows>(a, u);
+    Tile t;
+    if constexpr (SEEN == kListed) {
+        const int each = (a.group + kTileRows - 1) / kTileRows;
+        t = find_row<kTileRows>(a, u / each, u % each * kTileRows);
+    } else {
+        t = a.many ? tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2)
+                   : find_tile<kTileRows, SEEN>(a, u);
+    }
     if (t.pairs == 0 || (a.many && t.request_pairs >= kManyPairs)) return;
+    if (SEEN == kPrefix && (t.request >= a.n_groups || t.length == 0)) return;
+    const int from = SEEN == kOwn && t.request < a.requests ? request_prefix(a, t.request) : 0;       // the first token that is looked at
     const bool there = col < t.pairs;
     const int pair = t.pair0 + col, row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group, own = there ? a.positions[row] : -1;
     i32x4_t q[kQ];
@@ -269,24 +345,53 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
         q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + g * (DIM / 4) + s * 8, a.flip) : i32x4_t{0, 0, 0, 0};
     // Without a window the steps are those of the request's length, so that the first codes need not wait for the positions; the
     // last of them may be masked whole.
-    Steps steps = {t.length > 0 ? (t.length + kStep - 1) / kStep : 0, 0, 0};
-    if (a.window) {
+    Steps steps = {t.length > from ? (t.length + kStep - 1) / kStep - from / kStep : 0, 0, from / kStep, 0};
+    const int32_t *list = nullptr;                       // of this row and key head
+    int listed = 0, visible = 0;                         // places of it up to the last that is looked at; tokens that the row sees
+    if constexpr (SEEN == kListed) {
+        list = a.selected + ((int64_t)t.row0 * a.kv_heads + head) * a.keep;
+        visible = min(uniform(row_max(own)), t.length - 1) + 1;
+        for (int i = lane; i < a.keep && visible > 0; i += 64) {
+            const int block = list[i];
+            if (block >= 0 && (int64_t)block << a.block_log < visible) listed = i + 1;
+        }
+        listed = wave_max(listed);
+        steps.count = (int)((((int64_t)listed << a.block_log) + kStep - 1) / kStep);
+    } else if (a.window) {
         const int seeing = -uniform(row_max(own >= 0 ? -own : -0x7fffffff));
-        steps = steps_of<kStep>(a, seeing, uniform(row_max(own)), t.length);
+        steps = steps_of<kStep>(a, seeing, uniform(row_max(own)), t.length, from);
     }
-    const int each = steps_each(steps.count, a.splits), begin = split * each, end = min(steps.count, begin + each);
+    const int each = max(steps_each(steps.count, a.splits), SEEN == kAll ? 0 : kFewest / kStep), begin = split * each, end = min(steps.count, begin + each);
     if (split > 0 && begin >= end) return;
-    const bool whole = each >= steps.count;              // no other split has any steps
+    const bool whole = each >= steps.count && SEEN != kPrefix && from == 0;       // no other split, or launch, has any steps
 
-    const TableRow table = table_row(a, t.request);
+    const TableRow table = table_row(a, SEEN == kPrefix ? leader_of(a, t.request) : t.request);
     // the last step of this wavefront is loaded again where there is no next one: a load that some rounds leave out would
     // make every round wait for all that are on their way
     Held<DIM> held_a, held_b;
-    StepBlocks blocks = {{-1, -1}}, next_blocks = {{-1, -1}};
+    StepBlocks blocks = {{-1, -1}, {}}, next_blocks = {{-1, -1}, {}};
     const int first = begin + wave, last = first + (end - 1 - first) / kAttendWaves * kAttendWaves;
+    // Of a list, the blocks of 32 rounds at a time are looked up, two lanes a round: list and table are a chain that no round should wait for.
+    int entry_id = -1, entry_token = 0, entries_from = -1;
+    auto step_blocks = [&](int i) {
+        if constexpr (SEEN != kListed) return blocks_of(a, table, steps.at(i), t.length);
+        const int r = (i - first) / kAttendWaves;         // round of this wavefront
+        if ((r & ~31) != entries_from) {
+            entries_from = r & ~31;
+            const int token = (first + (entries_from + lane / 2) * kAttendWaves) * kStep + lane % 2 * 16, place = token >> a.block_log;
+            const int block = place < listed ? list[place] : -1;
+            const bool seen = block >= 0 && (int64_t)block << a.block_log < visible;
+            const int id = seen ? a.table[(int64_t)t.request * a.width + block] : -1;
+            entry_id = id < a.blocks ? id : -1;
+            entry_token = seen ? (block << a.block_log) + (token & ((1 << a.block_log) - 1)) : 0;
+        }
+        const int at = r % 32 * 2;
+        return StepBlocks{{max(__builtin_amdgcn_readlane(entry_id, at), -1), max(__builtin_amdgcn_readlane(entry_id, at + 1), -1)},
+                          {__builtin_amdgcn_readlane(entry_token, at), __builtin_amdgcn_readlane(entry_token, at + 1)}};
+    };
     if (first < end) {
-        blocks = blocks_of(a, table, steps.at(first), t.length);
-        next_blocks = blocks_of(a, table, steps.at(min(first + kAttendWaves, last)), t.length);
+        blocks = step_blocks(first);
+        next_blocks = step_blocks(min(first + kAttendWaves, last));
         load_step<DIM>(a, head, steps.at(first), blocks, held_a);
     }
     const int highest = uniform(row_max(own)), lowest = -uniform(row_max(there ? -max(own, -1) : -0x7fffffff));
@@ -302,7 +407,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
     auto round = [&](int i, Held<DIM> &held, Held<DIM> &next) {
         const int step = steps.at(i);
         load_step<DIM>(a, head, steps.at(min(i + kAttendWaves, last)), next_blocks, next);
-        const StepBlocks later = blocks_of(a, table, steps.at(min(i + 2 * kAttendWaves, last)), t.length);
+        const StepBlocks later = step_blocks(min(i + 2 * kAttendWaves, last));
         f32x4_t s[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -317,11 +422,13 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = in_twos(s[e / 4][e % 4], a.scale);
         const int token0 = step * kStep;
-        if (token0 + kStep - 1 > full_to || (token0 < full_from && token0 + kStep > a.sinks) || blocks.id[0] < 0 || blocks.id[1] < 0) {
+        const int sixteen[2] = {SEEN == kListed ? blocks.token[0] : token0, SEEN == kListed ? blocks.token[1] : token0 + 16};
+        if (max(sixteen[0], sixteen[1]) + 15 > full_to || (token0 < full_from && token0 + kStep > a.sinks) || (SEEN == kOwn && token0 < from) ||
+            blocks.id[0] < 0 || blocks.id[1] < 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int token = token0 + e / 4 * 16 + g * 4 + e % 4;
-                const bool seen = blocks.id[e / 4] >= 0 && token <= position && (token > last_sink || token < a.sinks);
+                const int token = sixteen[e / 4] + g * 4 + e % 4;
+                const bool seen = blocks.id[e / 4] >= 0 && token <= position && (token > last_sink || token < a.sinks) && (SEEN != kOwn || token >= from);
                 p[e] = seen ? p[e] : -INFINITY;
             }
             // codes and scales of what is not held may be anything: a weight of 0 needs a finite value beside it
@@ -329,7 +436,8 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const bool is = blocks.id[k] >= 0 && token0 + k * 16 + g * 4 + r < t.length;
+                    const int token = sixteen[k] + g * 4 + r;
+                    const bool is = blocks.id[k] >= 0 && token < t.length && (SEEN != kOwn || token >= from);
                     held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
                 }
         }
@@ -412,13 +520,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             }
             const int pr = t.pair0 + c;
             const int64_t out_row = (int64_t)(t.row0 + pr / a.group) * a.q_heads + head * a.group + pr % a.group;
-            float *part = a.parts + (out_row * a.splits + split) * (DIM + kPartExtra);
+            float *part = a.parts + (SEEN == kPrefix || SEEN == kOwn ? out_row * a.slots + a.first_slot + split : out_row * a.splits + split) * (DIM + kPartExtra);
             if (whole) static_cast<T *>(a.out)[out_row * DIM + half * (DIM / 2) + d] = (T)(l == 0 ? 0.f : v / l);
             else part[half * (DIM / 2) + d] = v;
-            if (half == 0 && d == 0 && a.splits > 1) {
+            if (half == 0 && d == 0 && (a.splits > 1 || SEEN == kPrefix || SEEN == kOwn)) {
                 part[DIM] = m;
                 part[DIM + 1] = l;
-                part[DIM + 2] = __builtin_bit_cast(float, whole ? 1 : (steps.count + each - 1) / each);
+                part[DIM + 2] = __builtin_bit_cast(float, whole || steps.count == 0 ? 1 : (steps.count + each - 1) / each);
+                part[DIM + 3] = __builtin_bit_cast(float, (int)(from > 0));
             }
         }
     }
@@ -474,7 +583,7 @@ template <int DIM> __device__ static inline void load_many(const char *block, ui
     }
 }
 
-template <int DT, int DIM>
+template <int DT, int DIM, int SEEN>
 __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_attend_many(AttendArgs a) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 16, kJ = DIM / 16, kD = DIM / 32;
@@ -484,8 +593,12 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     __shared__ i32x4_t keys[2][2][kQ][2][32], values[2][kD][4][2][32];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 32, half = lane / 32;
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % a.many_tiles, split = rest / a.many_tiles;
-    const Tile t = a.ordered ? find_longest<kManyRows>(a, u) : find_tile<kManyRows>(a, u);
-    if (t.pairs == 0 || (t.request < a.requests && t.request_pairs < kManyPairs)) return;
+    Tile t;
+    if constexpr (SEEN == kPrefix) t = find_tile<kManyRows, SEEN>(a, u);
+    else t = a.ordered ? find_longest<kManyRows>(a, u) : find_tile<kManyRows, SEEN>(a, u);
+    if (t.pairs == 0 || (SEEN != kPrefix && t.request < a.requests && t.request_pairs < kManyPairs)) return;
+    if (SEEN == kPrefix && (t.request >= a.n_groups || t.length == 0)) return;
+    const int from = SEEN == kOwn && t.request < a.requests ? request_prefix(a, t.request) : 0;       // the first token that is looked at
     // positions: of the tile for the steps, of the wavefront for its masks
     const int row0 = t.row0 + t.pair0 / a.group, rest0 = t.pair0 % a.group;       // row and head of the tile's first pair
     auto position_of = [&](int i) { return i < t.pairs ? a.positions[row0 + by_group(a, rest0 + i)] : -1; };
@@ -501,7 +614,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
 
     // The blocks of a step: lane l loads the entry of sixteen l % 4, through the vector unit, whose loads end in order (a scalar load on
     // its way would make every wait for the LDS one for all).  It is asked for three steps ahead, the codes two.
-    const int32_t *table = a.table + (int64_t)t.request * a.width;
+    const int32_t *table = a.table + (int64_t)(SEEN == kPrefix ? leader_of(a, t.request) : t.request) * a.width;
     auto token_of = [&](int step) { return step * kManyStep + lane % 4 * 16; };
     auto entry_at = [&](int step) { const int token = token_of(step); return table[token < t.length ? token >> a.block_log : 0]; };
     struct Blocks { int own, here; };                     // of the wavefront's sixteen, -1: none; a bit for each sixteen that has one
@@ -533,13 +646,14 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
         next = blocks_at(step_1, second);
         load(step, these.own);
     };
-    if (early && held_steps > 0) begin_at(0, min(1, held_steps - 1), min(2, held_steps - 1));
+    const int low = from / kManyStep;
+    if (early && t.length > from) begin_at(low, min(low + 1, held_steps - 1), min(low + 2, held_steps - 1));
     const int highest = wave_max(max(p0, p1));
     const int seeing = -wave_max(max(p0 >= 0 ? -p0 : -0x7fffffff, p1 >= 0 ? -p1 : -0x7fffffff));
-    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length);
-    const int each = (steps.count + a.splits - 1) / a.splits, begin = split * each, end = min(steps.count, begin + each);
+    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length, from);
+    const int each = max((steps.count + a.splits - 1) / a.splits, SEEN == kAll ? 0 : kFewest / kManyStep), begin = split * each, end = min(steps.count, begin + each);
     if (split > 0 && begin >= end) return;
-    const bool whole = each >= steps.count;
+    const bool whole = each >= steps.count && SEEN != kPrefix && from == 0;
     auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
     if (!early && begin < end) begin_at(steps.at(begin), clamped(begin + 1), clamped(begin + 2));
     const int own = __shfl(wave < 2 ? p0 : p1, wave % 2 * 32 + col);
@@ -557,12 +671,13 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     // what is not held may be anything: its values are to be finite, its scores are masked
     auto blank = [&](int step, int id) {
         const int g = lane / 16, h = g % 2, token0 = step * kManyStep + wave * 16;
-        if (id >= 0 && token0 + 16 <= t.length) return;
+        if (id >= 0 && token0 + 16 <= t.length && (SEEN != kOwn || token0 >= from)) return;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool is = id >= 0 && token0 + (h + 2 * k) * 4 + r < t.length;
+                const int token = token0 + (h + 2 * k) * 4 + r;
+                const bool is = id >= 0 && token < t.length && (SEEN != kOwn || token >= from);
                 held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
             }
     };
@@ -633,13 +748,14 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
         entry = entry_at(step_3);
         load(step_2, later.own);
         if (!idle && token0 <= min(wave_highest, t.length - 1)) {
-            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || these.here != 15) {
+            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || (SEEN == kOwn && token0 < from) || these.here != 15) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int token = token0 + b * 32 + 8 * (r / 4) + 4 * half + r % 4;
-                        const bool seen = (these.here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks);
+                        const bool seen = (these.here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks) &&
+                                          (SEEN != kOwn || token >= from);
                         s[b][r] = seen ? s[b][r] : -INFINITY;
                     }
             }
@@ -690,7 +806,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     if (!there) return;
     // lane: pair col, values 32 d + 8 (r / 4) + 4 half + r % 4
     const int64_t out_row = (int64_t)row * a.q_heads + qh;
-    float *parts = a.parts + (out_row * a.splits + split) * (DIM + kPartExtra);
+    float *parts = a.parts + (SEEN == kPrefix || SEEN == kOwn ? out_row * a.slots + a.first_slot + split : out_row * a.splits + split) * (DIM + kPartExtra);
     const float inverse = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
     for (int d = 0; d < kD; ++d)
@@ -706,10 +822,11 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
                 *reinterpret_cast<f32x4_t *>(parts + at) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
             }
         }
-    if (a.splits > 1 && half == 0) {
+    if ((a.splits > 1 || SEEN == kPrefix || SEEN == kOwn) && half == 0) {
         parts[DIM] = base;
         parts[DIM + 1] = sum;
-        parts[DIM + 2] = __builtin_bit_cast(float, whole ? 1 : (steps.count + each - 1) / each);
+        parts[DIM + 2] = __builtin_bit_cast(float, whole || steps.count == 0 ? 1 : (steps.count + each - 1) / each);
+        parts[DIM + 3] = __builtin_bit_cast(float, (int)(from > 0));
     }
 }
 
@@ -749,6 +866,53 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     f32x4_t v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int s = group; s < splits; s += kGroups) v += *reinterpret_cast<const f32x4_t *>(p + s * (DIM + kPartExtra) + 4 * at) * factor[s];
+    part[group][at] = v;
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) v += part[i][at];
+    ElemVec<DT, 4> y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (T)(l == 0 ? 0.f : v[i] / l);
+    *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + (int64_t)blockIdx.x * DIM + 4 * at) = y;
+}
+
+// Joins what the prefix's splits (the first a.first_slot slots of a row and query head) and its own (those behind) gave, as kv_attend_join.
+template <int DT, int DIM>
+__global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
+    typedef typename Elem<DT>::type T;
+    constexpr int kLanes = DIM / 4, kGroups = 256 / kLanes;
+    __shared__ float factor[256], bases[4], sums[4];
+    __shared__ f32x4_t part[kGroups][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float *p = a.parts + (int64_t)blockIdx.x * a.slots * (DIM + kPartExtra), *own = p + a.first_slot * (DIM + kPartExtra);
+    const bool slot = tid < a.slots;
+    const float own_base = slot ? p[tid * (DIM + kPartExtra) + DIM] : 0.f, own_sum = slot ? p[tid * (DIM + kPartExtra) + DIM + 1] : 0.f;
+    // (what is read of results that there are not is not used: a row that starts leave out may have any numbers)
+    const int own_count = max(min(__builtin_bit_cast(int, own[DIM + 2]), a.splits), 0);
+    const int count = __builtin_bit_cast(int, own[DIM + 3]) != 0 ? max(min(__builtin_bit_cast(int, p[DIM + 2]), a.first_slot), 0) : 0;
+    if (count + own_count <= 1 && count == 0) return;
+    const bool mine = tid < count || (tid >= a.first_slot && tid - a.first_slot < own_count);
+    const float base = mine ? own_base : -3.4028234663852886e38f;
+    float m = base;
+    for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
+    if (lane == 0) bases[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(bases[0], bases[1]), fmaxf(bases[2], bases[3]));
+    const float f = mine ? __builtin_amdgcn_exp2f(base - m) : 0.f;
+    float l = mine ? own_sum * f : 0.f;
+    for (int s = 1; s < 64; s *= 2) l += __shfl_xor(l, s);
+    if (lane == 0) sums[wave] = l;
+    factor[tid] = f;
+    __syncthreads();
+    l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    const int group = tid / kLanes, at = tid % kLanes;
+    f32x4_t v = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = group; i < count + own_count; i += kGroups) {
+        const int s = i < count ? i : a.first_slot + i - count;
+        v += *reinterpret_cast<const f32x4_t *>(p + s * (DIM + kPartExtra) + 4 * at) * factor[s];
+    }
     part[group][at] = v;
     __syncthreads();
     if (group) return;
@@ -801,11 +965,11 @@ size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, i
 
 template <int DT, int DIM> static hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t st) {
     if (a.many) {
-        kv_attend_many<DT, DIM><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
+        kv_attend_many<DT, DIM, kAll><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.tiles) kv_attend<DT, DIM><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
+    if (a.tiles) kv_attend<DT, DIM, kAll><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
@@ -826,6 +990,115 @@ hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &ar
     // the order costs a loop over the requests, and is for tiles that take many steps
     a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
     return d.dtype == NNV_F16 ? launch_attend_type<NNV_F16>(a, d.head_dim, st) : launch_attend_type<NNV_BF16>(a, d.head_dim, st);
+}
+
+// ---- a prefix read once for the requests that share it, and what each has behind it ------------------------------------------
+
+// Both are the kernels above; their partial results are joined by one that knows of both.  The prefix goes to kv_attend_many, which converts its codes once for
+// 128 pairs, where a group has that many on average as fill a wavefront of it.
+static bool prefix_many(const nnv_attention_desc &d, int rows, int groups) { return (int64_t)rows * (d.q_heads / d.kv_heads) >= (int64_t)kManyPairs * groups; }
+
+struct SharedSplits { int prefix, own; };
+static SharedSplits shared_splits(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens, each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
+    const int64_t pairs = (int64_t)rows * (d.q_heads / d.kv_heads);
+    const int64_t most = (capacity + kFewest - 1) / kFewest < kMostSplits ? (capacity + kFewest - 1) / kFewest : kMostSplits;
+    auto cut = [&](int64_t tiles, int64_t fill) {
+        int64_t s = (fill + tiles * d.kv_heads - 1) / (tiles * d.kv_heads);
+        s = s < most ? s : most;
+        while (s > 1 && (s * each > (int64_t)128 << 20 || s * kv_attention_groups(d, requests > groups ? requests : groups, rows) >= 1 << 24)) s = s / 2;
+        return (int)(s < 1 ? 1 : s);
+    };
+    const int64_t tile = prefix_many(d, rows, groups) ? kManyRows : kTileRows, full = pairs / tile, least = groups < rows ? groups : rows;
+    const int64_t own = pairs / (attend_many(d, requests, rows) ? kManyRows : kTileRows), least_own = requests < rows ? requests : rows;
+    return {groups ? cut(full > least ? full : least, 512) : 0, cut(own > least_own ? own : least_own > 0 ? least_own : 1, 1024)};
+}
+
+size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    const SharedSplits s = shared_splits(d, requests, rows, groups);
+    return (size_t)rows * d.q_heads * (s.prefix + s.own) * (d.head_dim + kPartExtra) * 4;
+}
+
+template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attention_desc &d, const AttendArgs &args, hipStream_t st) {
+    AttendArgs a = args;
+    const SharedSplits s = shared_splits(d, a.requests, a.rows, a.n_groups);
+    a.slots = s.prefix + s.own;
+    if (a.n_groups) {
+        AttendArgs p = a;
+        p.splits = s.prefix;
+        p.first_slot = 0;
+        p.many = p.ordered = 0;
+        p.many_tiles = attend_tiles(a.n_groups, a.rows, a.group, kManyRows);
+        p.tiles = attend_tiles(a.n_groups, a.rows, a.group, kTileRows);
+        if (prefix_many(d, a.rows, a.n_groups)) kv_attend_many<DT, DIM, kPrefix><<<(unsigned)(p.many_tiles * p.kv_heads * p.splits), 256, 0, st>>>(p);
+        else kv_attend<DT, DIM, kPrefix><<<(unsigned)(p.tiles * p.kv_heads * p.splits), 64 * kAttendWaves, 0, st>>>(p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    a.first_slot = s.prefix;
+    a.splits = s.own;
+    a.many = attend_many(d, a.requests, a.rows);
+    a.tiles = a.many ? 2 * a.requests : attend_tiles(a.requests, a.rows, a.group, kTileRows);
+    a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
+    a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
+    if (a.many) kv_attend_many<DT, DIM, kOwn><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.tiles) kv_attend<DT, DIM, kOwn><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    kv_attend_join_shared<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <int DT> static hipError_t launch_shared_type(const nnv_attention_desc &d, const AttendArgs &a, hipStream_t st) {
+    return d.head_dim == 64 ? launch_shared_dim<DT, 64>(d, a, st) : d.head_dim == 128 ? launch_shared_dim<DT, 128>(d, a, st) : launch_shared_dim<DT, 256>(d, a, st);
+}
+
+hipError_t launch_kv_attention_shared(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
+    AttendArgs a = args;
+    a.parts = static_cast<float *>(ws);
+    a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
+    return d.dtype == NNV_F16 ? launch_shared_type<NNV_F16>(d, a, st) : launch_shared_type<NNV_BF16>(d, a, st);
+}
+
+// ---- the blocks that a row and key head's list names -------------------------------------------------------------------------
+
+static int64_t listed_tiles(const nnv_attention_desc &d, int rows) { return (int64_t)rows * ((d.q_heads / d.kv_heads + kTileRows - 1) / kTileRows); }
+int64_t kv_attention_blocks_groups(const nnv_attention_desc &d, int rows) { return listed_tiles(d, rows) * d.kv_heads; }
+
+static int listed_splits(const nnv_attention_desc &d, int rows, int keep) {
+    const int64_t groups = kv_attention_blocks_groups(d, rows), most = ((int64_t)keep * d.block_tokens + kFewest - 1) / kFewest;
+    const int64_t each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
+    int64_t s = (1024 + groups - 1) / groups;
+    if (s > most) s = most;
+    if (s > kMostSplits) s = kMostSplits;
+    while (s > 1 && (s * each > (int64_t)256 << 20 || s * groups >= 1 << 24)) s = s / 2;
+    return (int)(s < 1 ? 1 : s);
+}
+
+size_t kv_attention_blocks_workspace_bytes(const nnv_attention_desc &d, int rows, int keep) {
+    const int s = listed_splits(d, rows, keep);
+    return s == 1 ? 0 : (size_t)rows * d.q_heads * s * (d.head_dim + kPartExtra) * 4;
+}
+
+template <int DT, int DIM> static hipError_t launch_listed_dim(const AttendArgs &a, hipStream_t st) {
+    kv_attend<DT, DIM, kListed><<<(unsigned)((int64_t)a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <int DT> static hipError_t launch_listed_type(const AttendArgs &a, int dim, hipStream_t st) {
+    return dim == 64 ? launch_listed_dim<DT, 64>(a, st) : dim == 128 ? launch_listed_dim<DT, 128>(a, st) : launch_listed_dim<DT, 256>(a, st);
+}
+
+hipError_t launch_kv_attention_blocks(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
+    AttendArgs a = args;
+    a.tiles = (int)listed_tiles(d, a.rows);
+    a.splits = listed_splits(d, a.rows, a.keep);
+    a.parts = static_cast<float *>(ws);
+    a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
+    return d.dtype == NNV_F16 ? launch_listed_type<NNV_F16>(a, d.head_dim, st) : launch_listed_type<NNV_BF16>(a, d.head_dim, st);
 }
 
 }  // namespace nnv

@@ -14,7 +14,7 @@
 
 namespace {
 
-PyObject *g_linear_type, *g_attention_type;                                     // handed over by setup_serving()
+PyObject *g_linear_type, *g_attention_type, *g_residual_type;                   // handed over by setup_serving()
 PyObject *g_desc_type, *g_fail, *g_slow_stream, *g_get_device, *g_raw_stream;    // handed over by setup()
 PyObject *g_data_ptr, *g_numel, *g_element_size, *g_cuda_stream;                 // interned names
 bool g_stream_ready = false;     // torch has initialised the device: the raw calls may be used
@@ -378,15 +378,110 @@ PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return finish(rc, "nnv_kv_attention");
 }
 
-// (LinearDesc type, AttentionDesc type)
+// (desc, requests, rows, table, starts, lengths, cache, bounds, stream)
+PyObject *kv_bounds(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows;
+    void *cache, *bounds, *st;
+    int32_t *table, *starts, *lengths;
+    if (!count_is(n, 9) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) ||
+        !as_address(a[3], &table) || !as_address(a[4], &starts) || !as_address(a[5], &lengths) || !as_address(a[6], &cache) ||
+        !as_address(a[7], &bounds) || !as_stream(a[8], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_bounds(&d, requests, rows, table, starts, lengths, cache, bounds, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_bounds");
+}
+
+// (desc, requests, rows, keep, first, last, q, table, starts, lengths, positions, bounds, selected, workspace, workspace_bytes, stream)
+PyObject *kv_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows, keep, first, last;
+    void *q, *bounds, *workspace, *st;
+    int32_t *table, *starts, *lengths, *positions, *selected;
+    size_t bytes;
+    if (!count_is(n, 16) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) ||
+        !as_int(a[3], &keep) || !as_int(a[4], &first) || !as_int(a[5], &last) || !as_address(a[6], &q) || !as_address(a[7], &table) ||
+        !as_address(a[8], &starts) || !as_address(a[9], &lengths) || !as_address(a[10], &positions) || !as_address(a[11], &bounds) ||
+        !as_address(a[12], &selected) || !as_address(a[13], &workspace) || !as_bytes(a[14], a[13], &bytes) || !as_stream(a[15], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_select(&d, requests, rows, keep, first, last, q, table, starts, lengths, positions, bounds, selected, workspace, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_select");
+}
+
+// (desc, requests, rows, keep, q, table, starts, lengths, positions, selected, cache, out, workspace, workspace_bytes, stream)
+PyObject *kv_attention_blocks(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows, keep;
+    void *q, *cache, *out, *workspace, *st;
+    int32_t *table, *starts, *lengths, *positions, *selected;
+    size_t bytes;
+    if (!count_is(n, 15) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) ||
+        !as_int(a[3], &keep) || !as_address(a[4], &q) || !as_address(a[5], &table) || !as_address(a[6], &starts) ||
+        !as_address(a[7], &lengths) || !as_address(a[8], &positions) || !as_address(a[9], &selected) || !as_address(a[10], &cache) ||
+        !as_address(a[11], &out) || !as_address(a[12], &workspace) || !as_bytes(a[13], a[12], &bytes) || !as_stream(a[14], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_attention_blocks(&d, requests, rows, keep, q, table, starts, lengths, positions, selected, cache, out, workspace, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_attention_blocks");
+}
+
+// (desc, requests, rows, n_groups, q, table, starts, lengths, positions, groups, shared, cache, out, workspace, workspace_bytes, stream)
+PyObject *kv_attention_shared(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_attention_desc d;
+    int requests, rows, n_groups;
+    void *q, *cache, *out, *workspace, *st;
+    int32_t *table, *starts, *lengths, *positions, *groups, *shared;
+    size_t bytes;
+    if (!count_is(n, 16) || !as_struct(a[0], g_attention_type, &d) || !as_int(a[1], &requests) || !as_int(a[2], &rows) ||
+        !as_int(a[3], &n_groups) || !as_address(a[4], &q) || !as_address(a[5], &table) || !as_address(a[6], &starts) ||
+        !as_address(a[7], &lengths) || !as_address(a[8], &positions) || !as_address(a[9], &groups) || !as_address(a[10], &shared) ||
+        !as_address(a[11], &cache) || !as_address(a[12], &out) || !as_address(a[13], &workspace) || !as_bytes(a[14], a[13], &bytes) ||
+        !as_stream(a[15], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_kv_attention_shared(&d, requests, rows, n_groups, q, table, starts, lengths, positions, groups, shared, cache, out, workspace, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_kv_attention_shared");
+}
+
+// (desc, m, x, ldx, y, ldy, post, gates, gate, ldg, index, pre, x_out, ldo, h, ldh, stream)
+PyObject *residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    nnv_residual_desc d;
+    int m, gates;
+    int64_t ldx, ldy, ldg, ldo, ldh;
+    void *x, *y, *gate, *x_out, *h, *st;
+    float *post, *pre;
+    int32_t *index;
+    if (!count_is(n, 17) || !as_struct(a[0], g_residual_type, &d) || !as_int(a[1], &m) || !as_address(a[2], &x) || !as_int64(a[3], &ldx) ||
+        !as_address(a[4], &y) || !as_int64(a[5], &ldy) || !as_address(a[6], &post) || !as_int(a[7], &gates) || !as_address(a[8], &gate) ||
+        !as_int64(a[9], &ldg) || !as_address(a[10], &index) || !as_address(a[11], &pre) || !as_address(a[12], &x_out) || !as_int64(a[13], &ldo) ||
+        !as_address(a[14], &h) || !as_int64(a[15], &ldh) || !as_stream(a[16], &st))
+        return nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = nnv_residual_norm(&d, m, x, ldx, y, ldy, post, gates, gate, ldg, index, pre, x_out, ldo, h, ldh, st);
+    Py_END_ALLOW_THREADS
+    return finish(rc, "nnv_residual_norm");
+}
+
+// (LinearDesc type, AttentionDesc type, ResidualDesc type)
 PyObject *setup_serving(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (!count_is(n, 2)) return nullptr;
-    PyObject **slots[2] = {&g_linear_type, &g_attention_type};
-    if (!PyType_Check(a[0]) || !PyType_Check(a[1])) {
+    if (!count_is(n, 3)) return nullptr;
+    PyObject **slots[3] = {&g_linear_type, &g_attention_type, &g_residual_type};
+    if (!PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
         PyErr_SetString(PyExc_TypeError, "the arguments are the descriptor types");
         return nullptr;
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
         Py_INCREF(a[i]);
         Py_XSETREF(*slots[i], a[i]);
     }
@@ -412,7 +507,8 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef g_methods[] = {NNV_METHOD(setup), NNV_METHOD(conv_forward), NNV_METHOD(conv_forward_relu), NNV_METHOD(conv_forward_static),
                            NNV_METHOD(conv_forward_grouped), NNV_METHOD(transform_weights), NNV_METHOD(transform_weights_grouped),
                            NNV_METHOD(cold_stack), NNV_METHOD(setup_serving), NNV_METHOD(linear_transform_weights), NNV_METHOD(linear_forward),
-                           NNV_METHOD(kv_plan), NNV_METHOD(qk_norm_rope), NNV_METHOD(kv_read), NNV_METHOD(kv_attention), {nullptr, nullptr, 0, nullptr}};
+                           NNV_METHOD(kv_plan), NNV_METHOD(qk_norm_rope), NNV_METHOD(kv_read), NNV_METHOD(kv_attention), NNV_METHOD(kv_bounds), NNV_METHOD(kv_select),
+                           NNV_METHOD(kv_attention_blocks), NNV_METHOD(kv_attention_shared), NNV_METHOD(residual_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nnvpy", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

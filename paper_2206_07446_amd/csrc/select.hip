@@ -1,0 +1,347 @@
+// What attention over selected blocks reads before it: the bounds of the blocks' keys, and of each row the blocks that its queries select by them.
+#include "nnv_internal.h"
+#include "serving.h"
+#include "lowbits.h"
+
+namespace nnv {
+
+namespace {
+
+// The last of `count` places at or before `at` (0 if there is none), places ascending: a wavefront compares 64 of them at a time.
+template <typename F> __device__ inline int last_place(int count, int64_t at, F place) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, span = count;
+    for (;;) {
+        const int each = (span + 63) / 64, i = lo + lane * each;
+        const bool mine = lane * each < span;
+        const int n = max(__builtin_popcountll(__ballot(mine && place(mine ? i : lo) <= at)), 1);
+        lo = __builtin_amdgcn_readfirstlane(lo + (n - 1) * each);
+        span = __builtin_amdgcn_readfirstlane(min(each, span - (n - 1) * each));
+        if (each == 1) return lo;
+    }
+}
+
+}  // namespace
+
+// ---- bounds -------------------------------------------------------------------------------------
+
+typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
+
+// bfloat16 pairs as 16-bit numbers of the same order, and back: the bits below the sign are turned where it is set.
+__device__ static inline uint32_t ordered(uint32_t pair) {
+    const i16x2_t sign = __builtin_bit_cast(i16x2_t, pair) >> 15;
+    return pair ^ (__builtin_bit_cast(uint32_t, sign) & 0x7fff7fffu);
+}
+__device__ static inline uint32_t larger(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2_t, a), __builtin_bit_cast(i16x2_t, b)));
+}
+
+// A wavefront takes a block's head.  A lane reads the 32 codes of one token that share a scale, 16 bytes, and keeps their largest values, and the largest of
+// their complements, which are the complements of the smallest: values of e2m1 have two significant bits, and bfloat16 holds them all as they are.  Lanes of other
+// tokens are then joined by halves: each step hands over half of what is left, so that 64 values over 16 lanes cost 30 exchanges and not 128.
+// Bound by what it reads where many blocks are touched, by the chain of starts, table and codes where one of each request is.
+template <int DIM>
+__global__ __launch_bounds__(256) void kv_bounds(BoundsArgs a) {
+    constexpr int kGroups = DIM / 32, kTokens = 64 / kGroups;      // lanes of a token, tokens of a round
+    const int lane = threadIdx.x & 63, g = lane % kGroups, place = lane / kGroups;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= (int64_t)a.units * a.kv_heads) return;
+    const int u = (int)(unit / a.kv_heads), head = (int)(unit % a.kv_heads);
+    auto start_of = [&](int i) { return min(max(a.starts[i], 0), a.rows); };
+    // f tokens touch at most f / block + 2 blocks
+    const int request = last_place(a.requests, u, [&](int i) { return (int64_t)(start_of(i) >> a.block_log) + 2 * (int64_t)i; });
+    const int start = start_of(request), fresh = start_of(request + 1) - start, block = 1 << a.block_log;
+    const int length = min(max(a.lengths[request], 0), a.width << a.block_log);
+    const int column = (max(length - fresh, 0) >> a.block_log) + (u - (start >> a.block_log) - 2 * request);
+    if (fresh <= 0 || u - (start >> a.block_log) - 2 * request < 0 || ((int64_t)column << a.block_log) >= length) return;
+    const int id = a.table[(int64_t)request * a.width + column];
+    if (id < 0 || id >= a.blocks) return;
+    const KvLayout at{DIM, block};
+    const char *keys = a.cache + ((int64_t)id * a.kv_heads + head) * at.head_bytes();
+    const int held = min(length - (column << a.block_log), block);
+    uint32_t v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = 0x80008000u;
+#pragma unroll 4
+    for (int t = place; t < held; t += kTokens) {
+        const i32x4_t codes = *reinterpret_cast<const i32x4_t *>(keys + t * (DIM / 2) + g * 16);
+        const uint32_t byte = (uint8_t)keys[at.key_scale_at() + t * kGroups + g];
+        const float scale = scale_of_byte(min(max(byte, 1u), kMostE2m1Byte<NNV_BF16>));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t pairs[4] = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 0)),
+                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 1)),
+                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 2)),
+                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 3))};
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const uint32_t x = ordered(pairs[p]);
+                v[w * 4 + p] = larger(v[w * 4 + p], x);
+                v[16 + w * 4 + p] = larger(v[16 + w * 4 + p], ~x);
+            }
+        }
+    }
+    // lane bit b of `place` chooses the half that a lane keeps: what is left of it starts at `from`
+    int from = 0;
+#pragma unroll
+    for (int count = 16, mask = kGroups; mask < 64; mask *= 2, count /= 2) {
+        const bool upper = lane & mask;
+#pragma unroll
+        for (int i = 0; i < count; ++i) {
+            const uint32_t keep = upper ? v[count + i] : v[i], send = upper ? v[i] : v[count + i];
+            v[i] = larger(keep, (uint32_t)__shfl_xor((int)send, mask));
+        }
+        from += upper ? count : 0;
+    }
+    constexpr int kLeft = 32 / kTokens;                              // pairs left to a lane: 1, 2 or 4
+    const bool low = from >= 16;
+    uint32_t *out = reinterpret_cast<uint32_t *>(a.bounds + (((int64_t)id * a.kv_heads + head) * 2 + low) * DIM + g * 32) + (from & 15);
+#pragma unroll
+    for (int i = 0; i < kLeft; ++i) out[i] = ordered(low ? ~v[i] : v[i]);
+}
+
+hipError_t launch_kv_bounds(const BoundsArgs &a, int dim, hipStream_t st) {
+    const unsigned groups = (unsigned)(((int64_t)a.units * a.kv_heads + 3) / 4);
+    if (dim == 64) kv_bounds<64><<<groups, 256, 0, st>>>(a);
+    else if (dim == 128) kv_bounds<128><<<groups, 256, 0, st>>>(a);
+    else kv_bounds<256><<<groups, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// ---- selection ----------------------------------------------------------------------------------
+
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
+// Numbers in the order of 64-bit keys; a NaN counts as -infinity.  Key 0 is no block's.
+__device__ static inline uint64_t key_of(double v) {
+    v = v == v ? v + 0.0 : -INFINITY;                                // (-0 as 0)
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    return bits >> 63 ? ~bits : bits | (uint64_t)1 << 63;
+}
+
+// Scores of a tile of whole rows with a head's blocks: max(q hi, q lo) is max(q, 0) hi + min(q, 0) lo, so that a score is one product over 2 DIM, on the
+// matrix cores in float64: 16 blocks x 4 values x 4 (one 4x4x4 instruction for each four blocks) or 16 query heads (16x16x4).  Lane l holds of block, and of query
+// head, l % 16 (l % 4) the eight values from 32 s + 8 (l / 16): products sum over values in any order.
+template <int DT, int DIM, int COLS>
+__global__ __launch_bounds__(256) void kv_scores(SelectArgs a) {
+    typedef typename Elem<DT>::type T;
+    constexpr int kSteps = DIM / 32;
+    typedef ElemVec<DT, 8> Q8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % COLS;
+    const int chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks, head = rest % a.kv_heads, u = rest / a.kv_heads;
+    auto start_of = [&](int i) { return min(max(a.starts[i], a.row0), a.row0 + a.rows); };
+    const int request = last_place(a.requests, u, [&](int i) { return (int64_t)(start_of(i) - a.row0) / a.tile_rows + i; });
+    const int start = start_of(request), end = start_of(request + 1), local = u - ((start - a.row0) / a.tile_rows + request);
+    const int tile0 = start + local * a.tile_rows, rows = min(end - tile0, a.tile_rows);
+    if (local < 0 || rows <= 0) return;
+    const int length = min(max(a.lengths[request], 0), a.width << a.block_log);
+    int last = -1;                                                   // last token that a row of the tile sees
+    for (int r = 0; r < rows; ++r) last = max(last, min(a.positions[tile0 + r], length - 1));
+    const int first_block = chunk * a.chunk_blocks, end_block = min(first_block + a.chunk_blocks, last < 0 ? 0 : (last >> a.block_log) + 1);
+    if (first_block >= end_block) return;
+    const int32_t *table = a.table + (int64_t)request * a.width;
+
+    auto load = [&](int b0, i32x4_t (&hi)[kSteps], i32x4_t (&lo)[kSteps]) {
+        const int b = b0 + lane % 16, id = b < end_block ? table[b] : -1;
+        const bool is = id >= 0 && id < a.blocks;
+        const __bf16 *p = a.bounds + ((int64_t)(is ? id : 0) * a.kv_heads + head) * 2 * DIM + g * 8;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            hi[s] = *reinterpret_cast<const i32x4_t *>(p + s * 32);
+            lo[s] = *reinterpret_cast<const i32x4_t *>(p + DIM + s * 32);
+        }
+        return is;
+    };
+    const int many = a.group <= COLS ? 1 : (a.group + COLS - 1) / COLS;      // products of a row's heads
+    const int window = min(a.group, COLS);                                    // columns of a row
+    for (int b0 = first_block + wave * 16; b0 < end_block; b0 += 64) {
+        i32x4_t hi[kSteps], lo[kSteps];
+        const bool is = load(b0, hi, lo);
+        f64x4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        for (int c = 0; c < many; ++c) {
+            const int pair = c * COLS + col, row = many == 1 ? pair / a.group : 0, h = many == 1 ? pair % a.group : pair;
+            const bool there = row < rows && h < a.group;
+            f64x4_t sum = {0, 0, 0, 0};
+            const T *q = static_cast<const T *>(a.q) + ((int64_t)(tile0 + (there ? row : 0)) * a.q_heads + head * a.group + (there ? h : 0)) * DIM + g * 8;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const Q8 q8 = *reinterpret_cast<const Q8 *>(q + s * 32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t wh = hi[s][e / 2], wl = lo[s][e / 2];
+                    const double x = (double)__builtin_bit_cast(float, e % 2 ? wh & 0xffff0000u : wh << 16);
+                    const double y = (double)__builtin_bit_cast(float, e % 2 ? wl & 0xffff0000u : wl << 16);
+                    const float f = a.flip ? -(float)q8[e] : (float)q8[e];
+                    const double up = (double)fmaxf(f, 0.f), down = (double)fminf(f, 0.f);
+                    if constexpr (COLS == 4) {
+                        sum[0] = __builtin_amdgcn_mfma_f64_4x4x4f64(x, up, sum[0], 0, 0, 0);
+                        sum[0] = __builtin_amdgcn_mfma_f64_4x4x4f64(y, down, sum[0], 0, 0, 0);
+                    } else {
+                        sum = __builtin_amdgcn_mfma_f64_16x16x4f64(x, up, sum, 0, 0, 0);
+                        sum = __builtin_amdgcn_mfma_f64_16x16x4f64(y, down, sum, 0, 0, 0);
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < (COLS == 4 ? 1 : 4); ++r) best[r] = there ? fmax(best[r], sum[r]) : best[r];
+        }
+        // over the columns of a row, into its first: windows of twice the width, then one that ends where the row does
+        const int width = many == 1 ? window : COLS;
+        const uint64_t valid = __ballot(is);
+#pragma unroll
+        for (int r = 0; r < (COLS == 4 ? 1 : 4); ++r) {
+            double v = best[r];
+            int w = 1;
+            for (; 2 * w <= width; w *= 2) v = fmax(v, __shfl(v, lane + w));
+            if (w < width) v = fmax(v, __shfl(v, lane + width - w));
+            // lane: 16x16x4 holds block 4 r + g, 4x4x4 block 4 (lane / 4 % 4) + g of query head lane % COLS
+            const int in = COLS == 4 ? lane / 4 % 4 * 4 + g : 4 * r + g, block = b0 + in;
+            const int row = many == 1 ? col / a.group : 0;
+            if (col == row * width && row < rows && block < end_block)
+                a.scores[((int64_t)(tile0 + row - a.row0) * a.kv_heads + head) * a.width + block] = valid >> in & 1 ? key_of(v) : 0;
+        }
+    }
+}
+
+// The `keep` largest keys of a row and head, the lowest blocks where keys are equal, in ascending order.  The smallest key kept is found bit by bit: each bit is one
+// count over the keys, which stay in registers.
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void kv_pick(SelectArgs a) {
+    constexpr int kWaves = THREADS / 64;
+    __shared__ int counts[2][EACH][kWaves];
+    __shared__ int total[2][kWaves];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int row = a.row0 + (int)(blockIdx.x / a.kv_heads), head = blockIdx.x % a.kv_heads;
+    const int request = last_place(a.requests + 1, row, [&](int i) { return (int64_t)a.starts[i]; });
+    const bool real = request < a.requests && a.starts[request] <= row;
+    const int length = real ? min(max(a.lengths[request], 0), a.width << a.block_log) : 0;
+    const int last = min(a.positions[row], length - 1), visible = last < 0 ? 0 : (last >> a.block_log) + 1;
+    const uint64_t *scores = a.scores + ((int64_t)(row - a.row0) * a.kv_heads + head) * a.width;
+    int32_t *out = a.selected + ((int64_t)row * a.kv_heads + head) * a.keep;
+    uint64_t key[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int b = j * THREADS + t;
+        key[j] = b < visible ? scores[b] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int b = j * THREADS + t;
+        if (key[j] && (b < a.first || b >= visible - a.last)) key[j] = ~(uint64_t)0;
+    }
+    int turn = 0;
+    auto count = [&](uint64_t least) {
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) n += __builtin_popcountll(__ballot(key[j] >= least));
+        if constexpr (kWaves == 1) return n;
+        if (lane == 0) total[turn][wave] = n;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += total[turn][w];
+        turn ^= 1;
+        return all;
+    };
+    uint64_t least = 1;
+    int kept = count(1);
+    if (kept > a.keep) {
+        least = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            const uint64_t next = least | (uint64_t)1 << bit;
+            const int n = count(next);
+            if (n < a.keep) continue;
+            least = next;
+            kept = n;
+            if (n == a.keep) break;
+        }
+    }
+    // of the keys that are `least`, so many more than fit are left out, the last ones
+    const int chosen = min(kept, a.keep);
+    const int above = kept > a.keep ? count(least + 1) : 0;         // (a key of all ones cannot be one too many: first + last <= keep)
+    const int equal = chosen - above;
+    // places: of an element, those chosen before it; of the elements before its own round and wavefront by counts in the LDS
+    auto places = [&](auto want, int which, int (&before)[EACH]) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            const uint64_t set = __ballot(want(j));
+            before[j] = __builtin_popcountll(set & (((uint64_t)1 << lane) - 1));
+            if (lane == 0) counts[which][j][wave] = __builtin_popcountll(set);
+        }
+        __syncthreads();
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (w == wave) before[j] += sum;
+                sum += counts[which][j][w];
+            }
+    };
+    int before[EACH];
+    bool take[EACH];
+    if (kept > a.keep) {
+        places([&](int j) { return key[j] == least; }, 0, before);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) take[j] = key[j] > least || (key[j] == least && before[j] < equal);
+    } else {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) take[j] = key[j] >= least;
+    }
+    places([&](int j) { return take[j]; }, 1, before);
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+        if (take[j]) out[before[j]] = j * THREADS + t;
+    for (int i = chosen + t; i < a.keep; i += THREADS) out[i] = -1;
+}
+
+constexpr int64_t kScoreBytes = (int64_t)256 << 20;
+
+// Rows whose scores are kept at a time.
+static int select_rows(const nnv_attention_desc &d, int rows) {
+    const int64_t each = (int64_t)d.kv_heads * d.table_blocks * 8, fit = kScoreBytes / each;
+    return (int)(fit < 1 ? 1 : fit < rows ? fit : rows);
+}
+size_t kv_select_workspace_bytes(const nnv_attention_desc &d, int rows) {
+    return (size_t)select_rows(d, rows) * d.kv_heads * d.table_blocks * 8;
+}
+
+template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs &args, int step, hipStream_t st) {
+    SelectArgs a = args;
+    const int all = a.rows;
+    const bool narrow = a.group <= 4 && all <= a.requests;           // a row a request: no more columns than one has
+    a.tile_rows = narrow || a.group > 16 ? 1 : 16 / a.group;
+    for (int row0 = 0; row0 < all; row0 += step) {
+        a.row0 = row0;
+        a.rows = all - row0 < step ? all - row0 : step;
+        const int64_t tiles = (int64_t)a.rows / a.tile_rows + a.requests;
+        int64_t blocks = 128;
+        while (tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) >= 1 << 24) blocks *= 2;
+        a.chunk_blocks = (int)blocks;
+        a.chunks = (int)((a.width + blocks - 1) / blocks);
+        const unsigned groups = (unsigned)(tiles * a.kv_heads * a.chunks);
+        if (a.requests) {
+            if (narrow) kv_scores<DT, DIM, 4><<<groups, 256, 0, st>>>(a);
+            else kv_scores<DT, DIM, 16><<<groups, 256, 0, st>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        const unsigned picks = (unsigned)a.rows * a.kv_heads;
+        if (a.width <= 512) kv_pick<64, 8><<<picks, 64, 0, st>>>(a);
+        else if (a.width <= 2048) kv_pick<256, 8><<<picks, 256, 0, st>>>(a);
+        else if (a.width <= 8192) kv_pick<1024, 8><<<picks, 1024, 0, st>>>(a);
+        else kv_pick<1024, 32><<<picks, 1024, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <int DT> static hipError_t launch_select_type(const SelectArgs &a, int dim, int step, hipStream_t st) {
+    return dim == 64 ? launch_select_dim<DT, 64>(a, step, st) : dim == 128 ? launch_select_dim<DT, 128>(a, step, st) : launch_select_dim<DT, 256>(a, step, st);
+}
+hipError_t launch_kv_select(const nnv_attention_desc &d, const SelectArgs &a, hipStream_t st) {
+    const int step = select_rows(d, a.rows);
+    return d.dtype == NNV_F16 ? launch_select_type<NNV_F16>(a, d.head_dim, step, st) : launch_select_type<NNV_BF16>(a, d.head_dim, step, st);
+}
+
+}  // namespace nnv

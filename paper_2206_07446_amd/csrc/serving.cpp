@@ -17,6 +17,9 @@ inline int finish(hipError_t e) { return e == hipSuccess ? NNV_OK : record_hip_e
 // Sizes that the kernels' grids can hold.
 constexpr int kMostLinearN = 1 << 22, kMostLinearK = 1 << 20, kMostLinearRows = 65535 * 16;
 constexpr int kMostRows = 1 << 24, kMostRequests = 1 << 20;
+constexpr int kMostResidual = 32768, kMostResidualRows = 1 << 22;      // (1024 threads a row: fewer than 2^32)
+constexpr int kMostKeep = 1 << 20;                     // (its tokens are counted in 32 bits)
+constexpr int64_t kMostStride = (int64_t)1 << 40;
 constexpr int64_t kMostGroups = (1 << 24) - 1;        // workgroups of 256: a launch has fewer than 2^32 threads
 
 int check_linear(const nnv_linear_desc *d) {
@@ -71,8 +74,51 @@ int check_attention(const nnv_attention_desc *d) {
     return NNV_OK;
 }
 
+AttendArgs attend_values(const nnv_attention_desc &desc, int n_requests, int n_rows, const void *q, const int32_t *block_table, const int32_t *starts,
+                         const int32_t *lengths, const int32_t *positions, const void *cache, void *out) {
+    AttendArgs a{};
+    a.q = q; a.table = block_table; a.starts = starts; a.lengths = lengths; a.positions = positions;
+    a.cache = static_cast<const char *>(cache); a.out = out;
+    a.requests = n_requests; a.rows = n_rows; a.q_heads = desc.q_heads; a.kv_heads = desc.kv_heads; a.group = desc.q_heads / desc.kv_heads;
+    a.block_log = log2_of(desc.block_tokens); a.blocks = desc.blocks; a.width = desc.table_blocks; a.window = desc.window;
+    a.sinks = (int)std::min((int64_t)desc.sinks, (int64_t)desc.table_blocks * desc.block_tokens);     // (no more than there can be: sums of it stay within 32 bits)
+    a.scale = std::fmax(std::fabs(desc.scale) * 1.4426950408889634f, 1e-30f);
+    a.flip = desc.scale < 0 ? (int)0x80008000u : 0;
+    return a;
+}
+
 int check_counts(int n_requests, int n_rows) {
     return n_requests < 0 || n_rows < 0 || n_requests > kMostRequests || n_rows > kMostRows ? NNV_E_ARG : NNV_OK;
+}
+
+// Calls of attention over selected blocks.
+int check_selecting(const nnv_attention_desc *d) {
+    if (const int rc = check_attention(d)) return rc;
+    return d->window ? NNV_E_UNSUPPORTED : NNV_OK;
+}
+
+// More workgroups than a launch can have, of either kernel of a selection, at the fewest that a size can be cut into.
+bool select_too_large(const nnv_attention_desc &d, int requests, int rows) {
+    return ((int64_t)rows + requests) * d.kv_heads > (int64_t)1 << 22;      // (1024 threads a row and key head)
+}
+
+// What an attention call takes, checked; out and the workspace lie apart from the inputs and each other.
+int attend_args(const nnv_attention_desc *desc, int n_requests, int n_rows, const void *q, const int32_t *block_table, const int32_t *starts,
+                const int32_t *lengths, const int32_t *positions, const void *cache, void *out, void *workspace, size_t workspace_bytes, size_t need,
+                AttendArgs &a) {
+    if (!q || !starts || !positions || !cache || !out || (n_requests && (!block_table || !lengths))) return NNV_E_NULL;
+    if (need && !workspace) return NNV_E_NULL;
+    if (workspace_bytes < need) return NNV_E_WORKSPACE;
+    if (off16(q) || off4(block_table) || off4(starts) || off4(lengths) || off4(positions) || off16(cache) || off16(out) || (need && off16(workspace)))
+        return NNV_E_ALIGN;
+    const size_t n = n_requests, r = n_rows, values = 2 * r * desc->q_heads * desc->head_dim;
+    const Bytes to(out, values), scratch(workspace, need);
+    for (const Bytes &in : {Bytes(q, values), Bytes(block_table, 4 * n * desc->table_blocks), Bytes(starts, 4 * (n + 1)), Bytes(lengths, 4 * n),
+                            Bytes(positions, 4 * r), Bytes(cache, nnv_kv_cache_bytes(desc))})
+        if (to.meets(in) || scratch.meets(in)) return NNV_E_ARG;
+    if (to.meets(scratch)) return NNV_E_ARG;
+    a = attend_values(*desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out);
+    return NNV_OK;
 }
 
 }  // namespace
@@ -187,15 +233,163 @@ int nnv_kv_attention(const nnv_attention_desc *desc, int n_requests, int n_rows,
     if (workspace_bytes < need) return NNV_E_WORKSPACE;
     if (off16(q) || off4(block_table) || off4(starts) || off4(lengths) || off4(positions) || off16(cache) || off16(out) || (need && off16(workspace)))
         return NNV_E_ALIGN;
-    AttendArgs a{};
-    a.q = q; a.table = block_table; a.starts = starts; a.lengths = lengths; a.positions = positions;
-    a.cache = static_cast<const char *>(cache); a.out = out;
-    a.requests = n_requests; a.rows = n_rows; a.q_heads = desc->q_heads; a.kv_heads = desc->kv_heads; a.group = desc->q_heads / desc->kv_heads;
-    a.block_log = log2_of(desc->block_tokens); a.blocks = desc->blocks; a.width = desc->table_blocks; a.window = desc->window;
-    a.sinks = (int)std::min((int64_t)desc->sinks, (int64_t)desc->table_blocks * desc->block_tokens);     // (no more than there can be: sums of it stay within 32 bits)
-    a.scale = std::fmax(std::fabs(desc->scale) * 1.4426950408889634f, 1e-30f);
-    a.flip = desc->scale < 0 ? (int)0x80008000u : 0;
+    const AttendArgs a = attend_values(*desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out);
     return finish(launch_kv_attention(*desc, a, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t nnv_kv_bounds_bytes(const nnv_attention_desc *desc) {
+    if (check_selecting(desc)) return 0;
+    return (size_t)desc->blocks * desc->kv_heads * 4 * desc->head_dim;
+}
+
+int nnv_kv_bounds(const nnv_attention_desc *desc, int n_requests, int n_rows, const int32_t *block_table, const int32_t *starts, const int32_t *lengths,
+                  const void *cache, void *bounds, void *hip_stream) {
+    if (const int rc = check_selecting(desc)) return rc;
+    if (const int rc = check_counts(n_requests, n_rows)) return rc;
+    if (n_requests == 0 || n_rows == 0) return NNV_OK;
+    const int log = log2_of(desc->block_tokens);
+    const int64_t units = (n_rows >> log) + 2 * (int64_t)n_requests;
+    if ((units * desc->kv_heads + 3) / 4 > kMostGroups) return NNV_E_ARG;
+    if (!block_table || !starts || !lengths || !cache || !bounds) return NNV_E_NULL;
+    if (off4(block_table) || off4(starts) || off4(lengths) || off16(cache) || off16(bounds)) return NNV_E_ALIGN;
+    const size_t n = n_requests;
+    const Bytes out(bounds, nnv_kv_bounds_bytes(desc));
+    for (const Bytes &in : {Bytes(block_table, 4 * n * desc->table_blocks), Bytes(starts, 4 * (n + 1)), Bytes(lengths, 4 * n), Bytes(cache, nnv_kv_cache_bytes(desc))})
+        if (out.meets(in)) return NNV_E_ARG;
+    BoundsArgs a{block_table, starts, lengths, static_cast<const char *>(cache), static_cast<__bf16 *>(bounds), n_requests, n_rows, desc->kv_heads, log,
+                 desc->blocks, desc->table_blocks, (int)units};
+    return finish(launch_kv_bounds(a, desc->head_dim, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t nnv_kv_select_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows) {
+    if (check_selecting(desc) || desc->table_blocks > kMostSelectBlocks || check_counts(n_requests, n_rows) || n_rows == 0 ||
+        select_too_large(*desc, n_requests, n_rows))
+        return 0;
+    return kv_select_workspace_bytes(*desc, n_rows);
+}
+
+int nnv_kv_select(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep, int n_first, int n_last, const void *q, const int32_t *block_table,
+                  const int32_t *starts, const int32_t *lengths, const int32_t *positions, const void *bounds, int32_t *selected, void *workspace,
+                  size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_selecting(desc)) return rc;
+    if (desc->table_blocks > kMostSelectBlocks) return NNV_E_UNSUPPORTED;
+    if (const int rc = check_counts(n_requests, n_rows)) return rc;
+    if (keep < 1 || keep > kMostKeep || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > keep) return NNV_E_ARG;
+    if (n_rows == 0) return NNV_OK;
+    if (select_too_large(*desc, n_requests, n_rows)) return NNV_E_ARG;
+    if (!q || !starts || !positions || !bounds || !selected || !workspace || (n_requests && (!block_table || !lengths))) return NNV_E_NULL;
+    const size_t need = kv_select_workspace_bytes(*desc, n_rows);
+    if (workspace_bytes < need) return NNV_E_WORKSPACE;
+    if (off16(q) || off4(block_table) || off4(starts) || off4(lengths) || off4(positions) || off16(bounds) || off4(selected) || off16(workspace)) return NNV_E_ALIGN;
+    const size_t n = n_requests, r = n_rows;
+    const Bytes out(selected, 4 * r * desc->kv_heads * keep), scratch(workspace, need);
+    for (const Bytes &in : {Bytes(q, 2 * r * desc->q_heads * desc->head_dim), Bytes(block_table, 4 * n * desc->table_blocks), Bytes(starts, 4 * (n + 1)),
+                            Bytes(lengths, 4 * n), Bytes(positions, 4 * r), Bytes(bounds, nnv_kv_bounds_bytes(desc))})
+        if (out.meets(in) || scratch.meets(in)) return NNV_E_ARG;
+    if (out.meets(scratch)) return NNV_E_ARG;
+    SelectArgs a{};
+    a.q = q; a.table = block_table; a.starts = starts; a.lengths = lengths; a.positions = positions; a.bounds = static_cast<const __bf16 *>(bounds);
+    a.selected = selected; a.scores = static_cast<uint64_t *>(workspace);
+    a.requests = n_requests; a.rows = n_rows; a.q_heads = desc->q_heads; a.kv_heads = desc->kv_heads; a.group = desc->q_heads / desc->kv_heads;
+    a.block_log = log2_of(desc->block_tokens); a.blocks = desc->blocks; a.width = desc->table_blocks; a.keep = keep; a.first = n_first; a.last = n_last;
+    a.flip = desc->scale < 0;
+    return finish(launch_kv_select(*desc, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t nnv_kv_attention_blocks_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep) {
+    if (check_selecting(desc) || check_counts(n_requests, n_rows) || n_rows == 0 || keep < 1 || keep > kMostKeep || kv_attention_blocks_groups(*desc, n_rows) > kMostGroups) return 0;
+    return kv_attention_blocks_workspace_bytes(*desc, n_rows, keep);
+}
+
+int nnv_kv_attention_blocks(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep, const void *q, const int32_t *block_table,
+                            const int32_t *starts, const int32_t *lengths, const int32_t *positions, const int32_t *selected, const void *cache, void *out,
+                            void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_selecting(desc)) return rc;
+    if (const int rc = check_counts(n_requests, n_rows)) return rc;
+    if (keep < 1 || keep > kMostKeep) return NNV_E_ARG;
+    if (n_rows == 0) return NNV_OK;
+    if (kv_attention_blocks_groups(*desc, n_rows) > kMostGroups) return NNV_E_ARG;
+    if (!selected) return NNV_E_NULL;
+    if (off4(selected)) return NNV_E_ALIGN;
+    const size_t need = kv_attention_blocks_workspace_bytes(*desc, n_rows, keep);
+    AttendArgs a;
+    if (const int rc = attend_args(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes, need, a)) return rc;
+    const Bytes list(selected, (size_t)4 * n_rows * desc->kv_heads * keep);
+    if (list.meets({out, (size_t)2 * n_rows * desc->q_heads * desc->head_dim}) || list.meets({workspace, need})) return NNV_E_ARG;
+    a.selected = selected; a.keep = keep;
+    return finish(launch_kv_attention_blocks(*desc, a, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t nnv_kv_attention_shared_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups) {
+    if (check_attention(desc) || check_counts(n_requests, n_rows) || n_rows == 0 || n_groups < 0 || n_groups > kMostRequests ||
+        kv_attention_groups(*desc, std::max(n_requests, n_groups), n_rows) > kMostGroups)
+        return 0;
+    return kv_attention_shared_workspace_bytes(*desc, n_requests, n_rows, n_groups);
+}
+
+int nnv_kv_attention_shared(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups, const void *q, const int32_t *block_table,
+                            const int32_t *starts, const int32_t *lengths, const int32_t *positions, const int32_t *groups, const int32_t *shared,
+                            const void *cache, void *out, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (const int rc = check_attention(desc)) return rc;
+    if (const int rc = check_counts(n_requests, n_rows)) return rc;
+    if (n_groups < 0 || n_groups > kMostRequests) return NNV_E_ARG;
+    if (n_rows == 0) return NNV_OK;
+    if (kv_attention_groups(*desc, std::max(n_requests, n_groups), n_rows) > kMostGroups) return NNV_E_ARG;
+    if (n_groups && (!groups || !shared)) return NNV_E_NULL;
+    if (off4(groups) || off4(shared)) return NNV_E_ALIGN;
+    const size_t need = kv_attention_shared_workspace_bytes(*desc, n_requests, n_rows, n_groups);
+    AttendArgs a;
+    if (const int rc = attend_args(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes, need, a)) return rc;
+    const size_t g = n_groups;
+    for (const Bytes &in : {Bytes(groups, g ? 4 * (g + 1) : 0), Bytes(shared, 4 * g)})
+        if (in.meets({out, (size_t)2 * n_rows * desc->q_heads * desc->head_dim}) || in.meets({workspace, need})) return NNV_E_ARG;
+    a.groups = groups; a.shared = shared; a.n_groups = n_requests ? n_groups : 0;
+    return finish(launch_kv_attention_shared(*desc, a, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+int nnv_residual_norm(const nnv_residual_desc *desc, int m, const void *x, int64_t ldx, const void *y, int64_t ldy, const float *post, int gates,
+                      const void *gate, int64_t ldg, const int32_t *index, const float *pre, void *x_out, int64_t ldo, void *h, int64_t ldh,
+                      void *hip_stream) {
+    if (!desc) return NNV_E_NULL;
+    const int64_t n = desc->n;
+    if (n <= 0 || n > kMostResidual) return NNV_E_BAD_DESC;
+    for (int t : {desc->x_dtype, desc->y_dtype, desc->h_dtype})
+        if (t != NNV_F32 && t != NNV_F16 && t != NNV_BF16) return NNV_E_BAD_DESC;
+    if (!std::isfinite(desc->scale) || !std::isfinite(desc->eps) || desc->eps < 0) return NNV_E_BAD_DESC;
+    if (m < 0 || m > kMostResidualRows) return NNV_E_ARG;
+    if (m == 0 || (!y && !pre)) return NNV_OK;
+    if (!x || (y && !x_out) || (pre && !h)) return NNV_E_NULL;
+    if (!y) post = nullptr, gate = nullptr, index = nullptr, x_out = nullptr;
+    if (!pre) h = nullptr;
+    if (!gate) index = nullptr;
+    if (gate && (gates < 1 || (!index && gates != 1 && gates < m))) return NNV_E_ARG;
+    if (m > 1 && (ldx < n || (y && (ldy < n || ldo < n)) || (pre && ldh < n))) return NNV_E_ARG;
+    if (gate && gates > 1 && ldg < n) return NNV_E_ARG;
+    for (int64_t ld : {ldx, ldy, ldg, ldo, ldh})
+        if (ld > kMostStride) return NNV_E_ARG;
+    if (off16(x) || off16(y) || off16(post) || off16(gate) || off4(index) || off16(pre) || off16(x_out) || off16(h)) return NNV_E_ALIGN;
+    const int xb = element_bytes(desc->x_dtype), yb = element_bytes(desc->y_dtype), hb = element_bytes(desc->h_dtype);
+    auto step = [&](int64_t ld, int bytes) { return m > 1 ? ld * bytes : 0; };
+    const Bytes x_row(x, n * xb), y_row(y, n * yb), o_row(x_out, n * xb), h_row(h, n * hb);
+    // what one row of threads writes, another may still have to read
+    auto whole = [](const Bytes &row, int64_t stride, int rows) { Bytes all = row; if (all.count) all.count += (size_t)stride * (rows - 1); return all; };
+    auto meets_shared = [&](const Bytes &row, int64_t stride) {      // weights, gates and indices
+        const Bytes all = whole(row, stride, m), gate_row(gate, n * yb);
+        return all.meets({post, (size_t)n * 4}) || all.meets({pre, (size_t)n * 4}) || all.meets({index, (size_t)m * 4}) ||
+               all.meets(whole(gate_row, gates > 1 ? ldg * yb : 0, gates));
+    };
+    if (x_out) {
+        const bool in_place = x_out == x && (m == 1 || ldo == ldx);
+        if (!in_place && rows_meet(m, o_row, step(ldo, xb), x_row, step(ldx, xb))) return NNV_E_ARG;
+        if (rows_meet(m, o_row, step(ldo, xb), y_row, step(ldy, yb)) || meets_shared(o_row, step(ldo, xb))) return NNV_E_ARG;
+    }
+    if (h) {
+        if (rows_meet(m, h_row, step(ldh, hb), x_row, step(ldx, xb)) || meets_shared(h_row, step(ldh, hb))) return NNV_E_ARG;
+        if (y && (rows_meet(m, h_row, step(ldh, hb), y_row, step(ldy, yb)) || rows_meet(m, h_row, step(ldh, hb), o_row, step(ldo, xb)))) return NNV_E_ARG;
+    }
+    ResidualArgs a{x, y, gate, post, pre, index, x_out, h, m > 1 ? ldx : 0, m > 1 ? ldy : 0, gates > 1 ? ldg : 0, m > 1 ? ldo : 0, m > 1 ? ldh : 0,
+                   m, (int)n, gates, desc->h_dtype, 0, desc->scale, desc->eps};
+    return finish(launch_residual_norm(*desc, a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -62,9 +62,49 @@ struct AttendArgs {
     uint32_t group_inverse;                    // 2^21 / group, rounded up
     float scale;        // magnitude of the factor of the scores, times log2(e); never 0, so that a score of -infinity stays one
     int flip;           // sign bits of a pair of 16-bit values where the factor is negative
+    const int32_t *groups, *shared, *selected;
+    int n_groups, keep;
+    int slots, first_slot;                     // partial results of a row and query head, and the first of this launch's (nnv_kv_attention_shared)
 };
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows);     // tiles of rows times key/value heads
 size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, int rows);
 hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &a, void *ws, hipStream_t st);
+size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups);
+hipError_t launch_kv_attention_shared(const nnv_attention_desc &d, const AttendArgs &a, void *ws, hipStream_t st);
+int64_t kv_attention_blocks_groups(const nnv_attention_desc &d, int rows);
+size_t kv_attention_blocks_workspace_bytes(const nnv_attention_desc &d, int rows, int keep);
+hipError_t launch_kv_attention_blocks(const nnv_attention_desc &d, const AttendArgs &a, void *ws, hipStream_t st);
+
+struct BoundsArgs {
+    const int32_t *table, *starts, *lengths;
+    const char *cache;
+    __bf16 *bounds;
+    int requests, rows, kv_heads, block_log, blocks, width, units;
+};
+hipError_t launch_kv_bounds(const BoundsArgs &a, int dim, hipStream_t st);
+
+struct SelectArgs {
+    const void *q;
+    const int32_t *table, *starts, *lengths, *positions;
+    const __bf16 *bounds;
+    int32_t *selected;
+    uint64_t *scores;
+    int requests, row0, rows, q_heads, kv_heads, group, block_log, blocks, width, keep, first, last;
+    int tile_rows, chunks, chunk_blocks, flip;
+};
+constexpr int kMostSelectBlocks = 32768;       // columns of the table: kv_pick holds the scores of all in registers
+size_t kv_select_workspace_bytes(const nnv_attention_desc &d, int rows);
+hipError_t launch_kv_select(const nnv_attention_desc &d, const SelectArgs &a, hipStream_t st);
+
+struct ResidualArgs {
+    const void *x, *y, *gate;
+    const float *post, *pre;
+    const int32_t *index;
+    void *x_out, *h;
+    int64_t ldx, ldy, ldg, ldo, ldh;
+    int m, n, gates, h_dtype, threads;         // threads: of a row
+    float scale, eps;
+};
+hipError_t launch_residual_norm(const nnv_residual_desc &d, const ResidualArgs &a, hipStream_t st);
 
 }  // namespace nnv
