@@ -7,17 +7,22 @@ namespace nnv {
 
 namespace {
 
-// The last of `count` places at or before `at` (0 if there is none), places ascending: a wavefront compares 64 of them at a time.
-template <typename F> __device__ inline int last_place(int count, int64_t at, F place) {
+// A request: its first row, the row behind its last, its tokens.
+struct Found { int request, start, end, length; };
+
+// The last of `count` requests whose place, which rises with its start, is at or before `at` (the first if there is none).  A wavefront compares 64 of them at a
+// time; what a request has beside its start comes with the last round, so that a chain of loads is one link long for up to 64 requests.
+template <typename S, typename P> __device__ inline Found last_place(int count, int64_t at, const int32_t *lengths, S start_of, P place) {
     const int lane = threadIdx.x & 63;
     int lo = 0, span = count;
     for (;;) {
-        const int each = (span + 63) / 64, i = lo + lane * each;
+        const int each = (span + 63) / 64, i = lane * each < span ? lo + lane * each : lo;
         const bool mine = lane * each < span;
-        const int n = max(__builtin_popcountll(__ballot(mine && place(mine ? i : lo) <= at)), 1);
+        const int start = start_of(i), end = each == 1 ? start_of(i + 1) : 0, length = each == 1 ? lengths[i] : 0;
+        const int n = max(__builtin_popcountll(__ballot(mine && place(i, start) <= at)), 1);
         lo = __builtin_amdgcn_readfirstlane(lo + (n - 1) * each);
         span = __builtin_amdgcn_readfirstlane(min(each, span - (n - 1) * each));
-        if (each == 1) return lo;
+        if (each == 1) return {lo, __builtin_amdgcn_readlane(start, n - 1), __builtin_amdgcn_readlane(end, n - 1), __builtin_amdgcn_readlane(length, n - 1)};
     }
 }
 
@@ -36,6 +41,22 @@ __device__ static inline uint32_t larger(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2_t, a), __builtin_bit_cast(i16x2_t, b)));
 }
 
+// Joins lanes that differ in bits MASK and up of their number, of 2 COUNT values each: of each pair one lane goes on with the lower half of the values, the other with
+// the upper.  -> where what is left lies among the values.
+template <int COUNT, int MASK> __device__ static inline int join_lanes(uint32_t (&v)[32], int lane) {
+    if constexpr (MASK >= 64) {
+        return 0;
+    } else {
+        const bool upper = lane & MASK;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const uint32_t keep = upper ? v[COUNT + i] : v[i], send = upper ? v[i] : v[COUNT + i];
+            v[i] = larger(keep, (uint32_t)__shfl_xor((int)send, MASK));
+        }
+        return (upper ? COUNT : 0) + join_lanes<COUNT / 2, MASK * 2>(v, lane);
+    }
+}
+
 // A wavefront takes a block's head.  A lane reads the 32 codes of one token that share a scale, 16 bytes, and keeps their largest values, and the largest of
 // their complements, which are the complements of the smallest: values of e2m1 have two significant bits, and bfloat16 holds them all as they are.  Lanes of other
 // tokens are then joined by halves: each step hands over half of what is left, so that 64 values over 16 lanes cost 30 exchanges and not 128.
@@ -49,9 +70,9 @@ __global__ __launch_bounds__(256) void kv_bounds(BoundsArgs a) {
     const int u = (int)(unit / a.kv_heads), head = (int)(unit % a.kv_heads);
     auto start_of = [&](int i) { return min(max(a.starts[i], 0), a.rows); };
     // f tokens touch at most f / block + 2 blocks
-    const int request = last_place(a.requests, u, [&](int i) { return (int64_t)(start_of(i) >> a.block_log) + 2 * (int64_t)i; });
-    const int start = start_of(request), fresh = start_of(request + 1) - start, block = 1 << a.block_log;
-    const int length = min(max(a.lengths[request], 0), a.width << a.block_log);
+    const Found f = last_place(a.requests, u, a.lengths, start_of, [&](int i, int start) { return (int64_t)(start >> a.block_log) + 2 * (int64_t)i; });
+    const int request = f.request, start = f.start, fresh = f.end - start, block = 1 << a.block_log;
+    const int length = min(max(f.length, 0), a.width << a.block_log);
     const int column = (max(length - fresh, 0) >> a.block_log) + (u - (start >> a.block_log) - 2 * request);
     if (fresh <= 0 || u - (start >> a.block_log) - 2 * request < 0 || ((int64_t)column << a.block_log) >= length) return;
     const int id = a.table[(int64_t)request * a.width + column];
@@ -62,37 +83,36 @@ __global__ __launch_bounds__(256) void kv_bounds(BoundsArgs a) {
     uint32_t v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = 0x80008000u;
-#pragma unroll 4
-    for (int t = place; t < held; t += kTokens) {
-        const i32x4_t codes = *reinterpret_cast<const i32x4_t *>(keys + t * (DIM / 2) + g * 16);
-        const uint32_t byte = (uint8_t)keys[at.key_scale_at() + t * kGroups + g];
-        const float scale = scale_of_byte(min(max(byte, 1u), kMostE2m1Byte<NNV_BF16>));
+    // four rounds are on their way together; behind the last token that one again, which changes nothing
+    for (int t0 = 0; t0 < held; t0 += 4 * kTokens) {
+        i32x4_t codes[4];
+        uint32_t byte[4];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t pairs[4] = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 0)),
-                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 1)),
-                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 2)),
-                                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[w], scale, 3))};
+        for (int i = 0; i < 4; ++i) {
+            const int t = min(t0 + i * kTokens + place, held - 1);
+            codes[i] = *reinterpret_cast<const i32x4_t *>(keys + t * (DIM / 2) + g * 16);
+            byte[i] = (uint8_t)keys[at.key_scale_at() + t * kGroups + g];
+        }
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const uint32_t x = ordered(pairs[p]);
-                v[w * 4 + p] = larger(v[w * 4 + p], x);
-                v[16 + w * 4 + p] = larger(v[16 + w * 4 + p], ~x);
+        for (int i = 0; i < 4; ++i) {
+            if (t0 + i * kTokens >= held) break;
+            const float scale = scale_of_byte(min(max(byte[i], 1u), kMostE2m1Byte<NNV_BF16>));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t pairs[4] = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i][w], scale, 0)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i][w], scale, 1)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i][w], scale, 2)),
+                                           __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i][w], scale, 3))};
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const uint32_t x = ordered(pairs[p]);
+                    v[w * 4 + p] = larger(v[w * 4 + p], x);
+                    v[16 + w * 4 + p] = larger(v[16 + w * 4 + p], ~x);
+                }
             }
         }
     }
-    // lane bit b of `place` chooses the half that a lane keeps: what is left of it starts at `from`
-    int from = 0;
-#pragma unroll
-    for (int count = 16, mask = kGroups; mask < 64; mask *= 2, count /= 2) {
-        const bool upper = lane & mask;
-#pragma unroll
-        for (int i = 0; i < count; ++i) {
-            const uint32_t keep = upper ? v[count + i] : v[i], send = upper ? v[i] : v[count + i];
-            v[i] = larger(keep, (uint32_t)__shfl_xor((int)send, mask));
-        }
-        from += upper ? count : 0;
-    }
+    const int from = join_lanes<16, kGroups>(v, lane);
     constexpr int kLeft = 32 / kTokens;                              // pairs left to a lane: 1, 2 or 4
     const bool low = from >= 16;
     uint32_t *out = reinterpret_cast<uint32_t *>(a.bounds + (((int64_t)id * a.kv_heads + head) * 2 + low) * DIM + g * 32) + (from & 15);
@@ -130,11 +150,11 @@ __global__ __launch_bounds__(256) void kv_scores(SelectArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % COLS;
     const int chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks, head = rest % a.kv_heads, u = rest / a.kv_heads;
     auto start_of = [&](int i) { return min(max(a.starts[i], a.row0), a.row0 + a.rows); };
-    const int request = last_place(a.requests, u, [&](int i) { return (int64_t)(start_of(i) - a.row0) / a.tile_rows + i; });
-    const int start = start_of(request), end = start_of(request + 1), local = u - ((start - a.row0) / a.tile_rows + request);
+    const Found f = last_place(a.requests, u, a.lengths, start_of, [&](int i, int start) { return (int64_t)((start - a.row0) / a.tile_rows) + i; });
+    const int request = f.request, start = f.start, end = f.end, local = u - ((start - a.row0) / a.tile_rows + request);
     const int tile0 = start + local * a.tile_rows, rows = min(end - tile0, a.tile_rows);
     if (local < 0 || rows <= 0) return;
-    const int length = min(max(a.lengths[request], 0), a.width << a.block_log);
+    const int length = min(max(f.length, 0), a.width << a.block_log);
     int last = -1;                                                   // last token that a row of the tile sees
     for (int r = 0; r < rows; ++r) last = max(last, min(a.positions[tile0 + r], length - 1));
     const int first_block = chunk * a.chunk_blocks, end_block = min(first_block + a.chunk_blocks, last < 0 ? 0 : (last >> a.block_log) + 1);
@@ -212,9 +232,9 @@ __global__ __launch_bounds__(THREADS) void kv_pick(SelectArgs a) {
     __shared__ int total[2][kWaves];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int row = a.row0 + (int)(blockIdx.x / a.kv_heads), head = blockIdx.x % a.kv_heads;
-    const int request = last_place(a.requests + 1, row, [&](int i) { return (int64_t)a.starts[i]; });
-    const bool real = request < a.requests && a.starts[request] <= row;
-    const int length = real ? min(max(a.lengths[request], 0), a.width << a.block_log) : 0;
+    Found f{};
+    if (a.requests) f = last_place(a.requests, row, a.lengths, [&](int i) { return a.starts[i]; }, [](int, int start) { return (int64_t)start; });
+    const int length = f.start <= row && row < f.end ? min(max(f.length, 0), a.width << a.block_log) : 0;
     const int last = min(a.positions[row], length - 1), visible = last < 0 ? 0 : (last >> a.block_log) + 1;
     const uint64_t *scores = a.scores + ((int64_t)(row - a.row0) * a.kv_heads + head) * a.width;
     int32_t *out = a.selected + ((int64_t)row * a.kv_heads + head) * a.keep;
