@@ -87,8 +87,8 @@ __device__ static inline int wave_max(int v) {
 __device__ static inline int by_group(const AttendArgs &a, int x) { return (int)((uint32_t)x * a.group_inverse >> 21); }
 
 // Which tokens the rows of a launch see: all of their request's; of a group of requests those that they have in common; of a request those behind the ones that it
-// has in common with others; or those of the blocks that a row and key head's list names.
-enum Seen { kAll, kPrefix, kOwn, kListed };
+// has in common with others; both of these; or those of the blocks that a row and key head's list names.
+enum Seen { kAll, kPrefix, kOwn, kListed, kBoth };
 
 // A tile of a request: R consecutive pairs of a row and a query head of the group.
 struct Tile {
@@ -107,22 +107,23 @@ __device__ static inline int prefix_of(const AttendArgs &a, int i) {
     const int leader = leader_of(a, i), held = leader < a.requests ? a.lengths[leader] : 0;
     return max(min(min(a.shared[i], held), capacity_of(a)), 0);
 }
-// Of a request; 0 where no group has it.
-__device__ static inline int request_prefix(const AttendArgs &a, int request) {
+// Of a request; no tokens where no group has it.
+struct Prefix { int tokens, leader; };
+__device__ static inline Prefix request_prefix(const AttendArgs &a, int request) {
     const int lane = threadIdx.x & 63;
     int lo = 0, span = a.n_groups;
     while (span > 0) {
         const int each = (span + 63) / 64, i = lo + lane * each;
         const bool mine = lane * each < span;
         const bool before = mine && leader_of(a, mine ? i : lo) <= request;
-        const int held = before && each == 1 && request < leader_of(a, i + 1) ? prefix_of(a, i) : 0;
+        const int held = before && each == 1 && request < leader_of(a, i + 1) ? prefix_of(a, i) : 0, leader = before && each == 1 ? leader_of(a, i) : 0;
         const int n = __builtin_popcountll(__ballot(before));
-        if (n == 0) return 0;
-        if (each == 1) return __builtin_amdgcn_readlane(held, n - 1);
+        if (n == 0) break;
+        if (each == 1) return {__builtin_amdgcn_readlane(held, n - 1), __builtin_amdgcn_readlane(leader, n - 1)};
         lo = uniform(lo + (n - 1) * each);
         span = uniform(min(each, span - (n - 1) * each));
     }
-    return 0;
+    return {0, 0};
 }
 
 // What a launch's rows are divided by: requests, or groups of them.
@@ -152,22 +153,67 @@ template <int R> __device__ static inline Tile tile_of(const AttendArgs &a, int 
 // Finds tile u.  Tiles of request i start at floor(starts[i] * group / R) + i: enough for its pairs, with gaps (pairs = 0); request `requests`
 // stands for the rows that belong to none.  Every wavefront does so by itself: 64 starts at a time are compared with u, and in the last round,
 // the only one of up to 63 requests, come with the starts after them and the lengths, so that a chain of loads is one link long.
-template <int R, int SEEN> __device__ static inline Tile find_tile(const AttendArgs &a, int u) {
+template <int R, int SEEN> __device__ static inline Tile find_tile(const AttendArgs &a, int u, Prefix *prefix) {
+    constexpr bool kBehind = SEEN == kOwn || SEEN == kBoth;
     const int lane = threadIdx.x & 63, units = units_of<SEEN>(a);
-    int lo = 0, span = units + 1;
+    auto place = [&](int start, int i) { return (int64_t)start * a.group / R + i; };
+    auto rest = [&](int start) { return tile_of<R>(a, units, start, a.rows, 0, u - place(start, units)); };
+    if (kBehind) *prefix = Prefix{0, 0};
+    if (units == 0) return rest(start_of<SEEN>(a, 0));
+    // (of up to 64 groups what they have in common comes with the requests' starts)
+    const bool grouped = kBehind && units <= 64 && a.n_groups <= 64, one = grouped && lane < a.n_groups;
+    const int first = one ? leader_of(a, lane) : 0x7fffffff, next = one ? leader_of(a, lane + 1) : 0, shared = one ? a.shared[lane] : 0;
+    int lo = 0, span = units;
     for (;;) {
         const int each = (span + 63) / 64, i = lo + lane * each;
-        const bool mine = lane * each < span, request = mine && i < units;
+        const bool mine = lane * each < span;
         const int start = mine ? start_of<SEEN>(a, i) : a.rows;
-        const int end = each == 1 && request ? start_of<SEEN>(a, i + 1) : a.rows, length = each == 1 && request ? length_of<SEEN>(a, i) : 0;
-        const int n = max(__builtin_popcountll(__ballot(mine && (int64_t)start * a.group / R + i <= u)), 1);
+        const int end = each == 1 && mine ? start_of<SEEN>(a, i + 1) : a.rows, length = each == 1 && mine ? length_of<SEEN>(a, i) : 0;
+        const int n = max(__builtin_popcountll(__ballot(mine && place(start, i) <= u)), 1);
         lo = uniform(lo + (n - 1) * each);
         span = uniform(min(each, span - (n - 1) * each));
-        if (each == 1) {
-            const int at = uniform(n - 1), from = __builtin_amdgcn_readlane(start, at);
-            return tile_of<R>(a, lo, from, __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(length, at), u - ((int64_t)from * a.group / R + lo));
+        if (each > 1) continue;
+        const int at = uniform(n - 1), from = __builtin_amdgcn_readlane(start, at), to = __builtin_amdgcn_readlane(end, at);
+        if (lo == units - 1 && u >= place(to, units)) return rest(to);
+        if (grouped) {
+            const int g = __builtin_popcountll(__ballot(first <= lo)) - 1;
+            if (g >= 0 && lo < __builtin_amdgcn_readlane(next, g)) {
+                const int leader = __builtin_amdgcn_readlane(first, g), held = __builtin_amdgcn_readlane(length, leader);
+                *prefix = Prefix{max(min(min(__builtin_amdgcn_readlane(shared, g), held), capacity_of(a)), 0), leader};
+            }
+        } else if (kBehind) {
+            *prefix = request_prefix(a, lo);
         }
+        return tile_of<R>(a, lo, from, to, __builtin_amdgcn_readlane(length, at), u - place(from, lo));
     }
+}
+
+// A part of a group's tile over its prefix: of `splits` parts the one of number `split`.
+struct Part { Tile tile; int split, splits; };
+
+// Part u of a key head.  Groups differ in rows and in prefixes: their tiles are cut so that parts have as many steps of S tokens each (a.prefix_units of them in all
+// and one more of each tile at most), which every wavefront works out by itself, a lane to a group.  More than 64 groups have tiles enough, cut alike.
+template <int R, int S> __device__ static inline Part find_part(const AttendArgs &a, int u) {
+    if (a.n_groups > 64) return {find_tile<R, kPrefix>(a, u / a.prefix_splits, nullptr), u % a.prefix_splits, a.prefix_splits};
+    const int lane = threadIdx.x & 63;
+    const bool mine = lane < a.n_groups;
+    const int start = mine ? start_of<kPrefix>(a, lane) : 0, end = mine ? start_of<kPrefix>(a, lane + 1) : 0, tokens = mine ? prefix_of(a, lane) : 0;
+    const int tiles = (int)((max((int64_t)(end - start) * a.group, (int64_t)0) + R - 1) / R), steps = (tokens + S - 1) / S;
+    float total = (float)tiles * (float)steps;
+    for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
+    // (rounded up by more than the sum is off: no more parts than there are workgroups)
+    const int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / a.prefix_units), 1e9f));
+    const int splits = min((steps + each - 1) / each, a.prefix_splits), parts = tiles * splits;
+    int before = 0, sum = parts;
+    for (int s = 1; s < 64; s *= 2) {
+        const int other = __shfl_up(sum, s);
+        sum += lane >= s ? other : 0;
+    }
+    before = sum - parts;
+    const uint64_t found = __ballot(before <= u && u < sum);
+    if (!found) return {};
+    const int at = __builtin_ctzll(found), local = u - __builtin_amdgcn_readlane(before, at), of = __builtin_amdgcn_readlane(splits, at);
+    return {tile_of<R>(a, at, __builtin_amdgcn_readlane(start, at), __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(tokens, at), local / of), local % of, of};
 }
 
 // Tile u of up to 63 requests with those of the longest requests first, and of each the last: every lane adds up the tiles of the
@@ -233,6 +279,23 @@ template <int S> __device__ static inline Steps steps_of(const AttendArgs &a, in
     s.count = end_token > from ? s.sinks + max(0, end - s.first) : 0;
     return s;
 }
+
+// The steps that a workgroup goes through.  BOTH: first those of the prefix, then those behind it; one that the two share inside is gone through twice, and a bit says
+// for which of them.
+constexpr int kOwnStep = 1 << 30;
+template <bool BOTH> struct Walk {
+    Steps common, own;
+    int count;
+    __device__ int at(int i) const {
+        if constexpr (!BOTH) return own.at(i);
+        return i < common.count ? common.at(i) : own.at(i - common.count) | kOwnStep;
+    }
+    __device__ void sum() { count = BOTH ? common.count + own.count : own.count; }
+};
+// Of a step of a tile whose first `from` tokens are common: its number, and the tokens that are looked at.
+template <int SEEN> __device__ static inline int number_of(int step) { return SEEN == kBoth ? step & (kOwnStep - 1) : step; }
+template <int SEEN> __device__ static inline int least_of(int step, int from) { return SEEN == kOwn ? from : SEEN == kBoth && step & kOwnStep ? from : 0; }
+template <int SEEN> __device__ static inline int end_of(int step, int from, int length) { return SEEN == kBoth && !(step & kOwnStep) ? from : length; }
 
 // Steps of a split: whole rounds of the wavefronts.
 __device__ static inline int steps_each(int steps, int splits) {
@@ -316,27 +379,43 @@ constexpr int kFewest = 512;       // tokens of a split at least, where the host
 // A column's scores are taken relative to a base that all its lanes share.  It need not be the maximum: it is raised,
 // and what was summed is scaled down, only when a weight of the wavefront would pass the most of WeightRange, which past the
 // first steps is hardly ever.
-template <int DT, int DIM, int SEEN>
-__global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_attend(AttendArgs a) {
+template <int DIM> using FewJoin = float[kAttendWaves][kTileRows][DIM / 2 + 4];
+using FewSums = float[kAttendWaves][kTileRows];
+
+template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(const AttendArgs &a, int group, FewJoin<DIM> &join, FewSums &join_base, FewSums &join_sum) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 32, kJ = DIM / 16;          // instructions of a score, of an output
-    __shared__ float join[kAttendWaves][kTileRows][DIM / 2 + 4];
-    __shared__ float join_base[kAttendWaves][kTileRows], join_sum[kAttendWaves][kTileRows];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 16, g = lane / 16;
-    const int u = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles, head = rest % a.kv_heads, split = rest / a.kv_heads;
+    int head, split, splits;
+    Tile t;
+    Prefix prefix = {0, 0};
     // beside kv_attend_many, requests of fewer than 32 pairs: two tiles each
     static_assert(kManyPairs <= 2 * kTileRows, "two tiles hold them");
-    Tile t;
-    if constexpr (SEEN == kListed) {
-        const int each = (a.group + kTileRows - 1) / kTileRows;
-        t = find_row<kTileRows>(a, u / each, u % each * kTileRows);
+    if constexpr (SEEN == kPrefix) {
+        const Part part = find_part<kTileRows, kStep>(a, group / a.kv_heads);
+        t = part.tile;
+        split = part.split;
+        splits = part.splits;
+        head = group % a.kv_heads;
     } else {
-        t = a.many ? tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2)
-                   : find_tile<kTileRows, SEEN>(a, u);
+        const int u = group % a.tiles, rest = group / a.tiles;
+        head = rest % a.kv_heads;
+        split = rest / a.kv_heads;
+        splits = a.splits;
+        if constexpr (SEEN == kListed) {
+            const int each = (a.group + kTileRows - 1) / kTileRows;
+            t = find_row<kTileRows>(a, u / each, u % each * kTileRows);
+        } else if (a.many) {
+            t = tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2);
+            if (SEEN == kOwn || SEEN == kBoth) prefix = request_prefix(a, u / 2);
+        } else {
+            t = find_tile<kTileRows, SEEN>(a, u, &prefix);
+        }
     }
     if (t.pairs == 0 || (a.many && t.request_pairs >= kManyPairs)) return;
     if (SEEN == kPrefix && (t.request >= a.n_groups || t.length == 0)) return;
-    const int from = SEEN == kOwn && t.request < a.requests ? request_prefix(a, t.request) : 0;       // the first token that is looked at
+    constexpr bool kBehind = SEEN == kOwn || SEEN == kBoth;
+    const int from = kBehind ? prefix.tokens : 0;        // the request's own tokens begin here
     const bool there = col < t.pairs;
     const int pair = t.pair0 + col, row = t.row0 + pair / a.group, qh = head * a.group + pair % a.group, own = there ? a.positions[row] : -1;
     i32x4_t q[kQ];
@@ -345,7 +424,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
         q[s] = there ? query_words(static_cast<const T *>(a.q) + ((int64_t)row * a.q_heads + qh) * DIM + g * (DIM / 4) + s * 8, a.flip) : i32x4_t{0, 0, 0, 0};
     // Without a window the steps are those of the request's length, so that the first codes need not wait for the positions; the
     // last of them may be masked whole.
-    Steps steps = {t.length > from ? (t.length + kStep - 1) / kStep - from / kStep : 0, 0, from / kStep, 0};
+    Walk<SEEN == kBoth> steps{{(from + kStep - 1) / kStep, 0, 0, 0}, {t.length > from ? (t.length + kStep - 1) / kStep - from / kStep : 0, 0, from / kStep, 0}, 0};
     const int32_t *list = nullptr;                       // of this row and key head
     int listed = 0, visible = 0;                         // places of it up to the last that is looked at; tokens that the row sees
     if constexpr (SEEN == kListed) {
@@ -356,14 +435,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             if (block >= 0 && (int64_t)block << a.block_log < visible) listed = i + 1;
         }
         listed = wave_max(listed);
-        steps.count = (int)((((int64_t)listed << a.block_log) + kStep - 1) / kStep);
+        steps.own.count = (int)((((int64_t)listed << a.block_log) + kStep - 1) / kStep);
     } else if (a.window) {
         const int seeing = -uniform(row_max(own >= 0 ? -own : -0x7fffffff));
-        steps = steps_of<kStep>(a, seeing, uniform(row_max(own)), t.length, from);
+        steps.own = steps_of<kStep>(a, seeing, uniform(row_max(own)), t.length, from);
+        if (SEEN == kBoth) steps.common = steps_of<kStep>(a, seeing, uniform(row_max(own)), from, 0);
     }
-    const int each = max(steps_each(steps.count, a.splits), SEEN == kAll ? 0 : kFewest / kStep), begin = split * each, end = min(steps.count, begin + each);
+    steps.sum();
+    const int each = max(steps_each(steps.count, splits), SEEN == kOwn || SEEN == kListed ? kFewest / kStep : 0), begin = split * each, end = min(steps.count, begin + each);
     if (split > 0 && begin >= end) return;
-    const bool whole = each >= steps.count && SEEN != kPrefix && from == 0;       // no other split, or launch, has any steps
+    const bool whole = each >= steps.count && SEEN != kPrefix && (SEEN != kOwn || from == 0);      // no other split, or launch, has any steps
 
     const TableRow table = table_row(a, SEEN == kPrefix ? leader_of(a, t.request) : t.request);
     // the last step of this wavefront is loaded again where there is no next one: a load that some rounds leave out would
@@ -374,7 +455,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
     // Of a list, the blocks of 32 rounds at a time are looked up, two lanes a round: list and table are a chain that no round should wait for.
     int entry_id = -1, entry_token = 0, entries_from = -1;
     auto step_blocks = [&](int i) {
-        if constexpr (SEEN != kListed) return blocks_of(a, table, steps.at(i), t.length);
+        if constexpr (SEEN == kBoth) {
+            const int step = steps.at(i);
+            return blocks_of(a, step & kOwnStep ? table : table_row(a, prefix.leader), number_of<SEEN>(step), end_of<SEEN>(step, from, t.length));
+        } else if constexpr (SEEN != kListed) {
+            return blocks_of(a, table, steps.at(i), t.length);
+        }
         const int r = (i - first) / kAttendWaves;         // round of this wavefront
         if ((r & ~31) != entries_from) {
             entries_from = r & ~31;
@@ -392,21 +478,22 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
     if (first < end) {
         blocks = step_blocks(first);
         next_blocks = step_blocks(min(first + kAttendWaves, last));
-        load_step<DIM>(a, head, steps.at(first), blocks, held_a);
+        load_step<DIM>(a, head, number_of<SEEN>(steps.at(first)), blocks, held_a);
     }
     const int highest = uniform(row_max(own)), lowest = -uniform(row_max(there ? -max(own, -1) : -0x7fffffff));
-    const int position = min(own, t.length - 1), last_sink = a.window ? own - a.window : -1;    // tokens up to this one are seen as sinks only
+    const int tokens = SEEN == kBoth ? max(t.length, from) : t.length;
+    const int position = min(own, tokens - 1), last_sink = a.window ? own - a.window : -1;    // tokens up to this one are seen as sinks only
     f32x4_t o[kJ];
 #pragma unroll
     for (int j = 0; j < kJ; ++j) o[j] = f32x4_t{0, 0, 0, 0};
     float base = -3.4028234663852886e38f, sum = 0;
-    const int full_to = min(lowest, t.length - 1);                       // steps that end here or before are seen by all rows,
+    const int full_to = min(lowest, tokens - 1);                         // steps that end here or before are seen by all rows,
     const int full_from = a.window ? highest - a.window + 1 : 0;        // if they begin here or behind
 
     __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
     auto round = [&](int i, Held<DIM> &held, Held<DIM> &next) {
         const int step = steps.at(i);
-        load_step<DIM>(a, head, steps.at(min(i + kAttendWaves, last)), next_blocks, next);
+        load_step<DIM>(a, head, number_of<SEEN>(steps.at(min(i + kAttendWaves, last))), next_blocks, next);
         const StepBlocks later = step_blocks(min(i + 2 * kAttendWaves, last));
         f32x4_t s[2];
 #pragma unroll
@@ -421,14 +508,15 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = in_twos(s[e / 4][e % 4], a.scale);
-        const int token0 = step * kStep;
+        const int token0 = number_of<SEEN>(step) * kStep, least = least_of<SEEN>(step, from), limit = end_of<SEEN>(step, from, t.length);
         const int sixteen[2] = {SEEN == kListed ? blocks.token[0] : token0, SEEN == kListed ? blocks.token[1] : token0 + 16};
-        if (max(sixteen[0], sixteen[1]) + 15 > full_to || (token0 < full_from && token0 + kStep > a.sinks) || (SEEN == kOwn && token0 < from) ||
-            blocks.id[0] < 0 || blocks.id[1] < 0) {
+        if (max(sixteen[0], sixteen[1]) + 15 > full_to || (token0 < full_from && token0 + kStep > a.sinks) ||
+            (kBehind && (token0 < least || token0 + kStep > limit)) || blocks.id[0] < 0 || blocks.id[1] < 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int token = sixteen[e / 4] + g * 4 + e % 4;
-                const bool seen = blocks.id[e / 4] >= 0 && token <= position && (token > last_sink || token < a.sinks) && (SEEN != kOwn || token >= from);
+                const bool seen = blocks.id[e / 4] >= 0 && token <= position && (token > last_sink || token < a.sinks) &&
+                                  (!kBehind || (token >= least && token < limit));
                 p[e] = seen ? p[e] : -INFINITY;
             }
             // codes and scales of what is not held may be anything: a weight of 0 needs a finite value beside it
@@ -437,7 +525,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int token = sixteen[k] + g * 4 + r;
-                    const bool is = blocks.id[k] >= 0 && token < t.length && (SEEN != kOwn || token >= from);
+                    const bool is = blocks.id[k] >= 0 && token < limit && (!kBehind || token >= least);
                     held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
                 }
         }
@@ -520,10 +608,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             }
             const int pr = t.pair0 + c;
             const int64_t out_row = (int64_t)(t.row0 + pr / a.group) * a.q_heads + head * a.group + pr % a.group;
-            float *part = a.parts + (SEEN == kPrefix || SEEN == kOwn ? out_row * a.slots + a.first_slot + split : out_row * a.splits + split) * (DIM + kPartExtra);
+            float *part = a.parts + (SEEN == kPrefix ? out_row * a.slots + split : SEEN == kOwn ? out_row * a.slots + a.prefix_splits + split : out_row * a.splits + split) * (DIM + kPartExtra);
             if (whole) static_cast<T *>(a.out)[out_row * DIM + half * (DIM / 2) + d] = (T)(l == 0 ? 0.f : v / l);
             else part[half * (DIM / 2) + d] = v;
-            if (half == 0 && d == 0 && (a.splits > 1 || SEEN == kPrefix || SEEN == kOwn)) {
+            if (half == 0 && d == 0 && (splits > 1 || SEEN == kPrefix || SEEN == kOwn)) {
                 part[DIM] = m;
                 part[DIM + 1] = l;
                 part[DIM + 2] = __builtin_bit_cast(float, whole || steps.count == 0 ? 1 : (steps.count + each - 1) / each);
@@ -531,6 +619,13 @@ __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_atte
             }
         }
     }
+}
+
+template <int DT, int DIM, int SEEN>
+__global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_attend(AttendArgs a) {
+    __shared__ FewJoin<DIM> join;
+    __shared__ FewSums join_base, join_sum;
+    attend_few<DT, DIM, SEEN>(a, blockIdx.x, join, join_base, join_sum);
 }
 
 // Requests of many rows: a workgroup holds 128 pairs, 32 to a wavefront, and goes over the tokens 64 at a time.  Each wavefront turns the codes of 16
@@ -583,22 +678,40 @@ template <int DIM> __device__ static inline void load_many(const char *block, ui
     }
 }
 
-template <int DT, int DIM, int SEEN>
-__global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_attend_many(AttendArgs a) {
+template <int DIM> using ManyKeys = i32x4_t[2][2][DIM / 16][2][32];
+template <int DIM> using ManyValues = i32x4_t[2][DIM / 32][4][2][32];
+
+template <int DT, int DIM, int SEEN> __device__ static inline void attend_many_rows(const AttendArgs &a, int group, ManyKeys<DIM> &keys, ManyValues<DIM> &values) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 16, kJ = DIM / 16, kD = DIM / 32;
     // Which part of a step goes before other wavefronts' work (4 prompts of 1024 rows, 4096 pairs each: heads of 64 scores 241 us, weights and outputs 262,
     // neither 256; of 128 210, 205, 208; of 256 362 all).
     constexpr bool kScoresFirst = DIM == 64;
-    __shared__ i32x4_t keys[2][2][kQ][2][32], values[2][kD][4][2][32];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 32, half = lane / 32;
-    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % a.many_tiles, split = rest / a.many_tiles;
+    const int head = group % a.kv_heads, rest = group / a.kv_heads;
+    int split, splits;
     Tile t;
-    if constexpr (SEEN == kPrefix) t = find_tile<kManyRows, SEEN>(a, u);
-    else t = a.ordered ? find_longest<kManyRows>(a, u) : find_tile<kManyRows, SEEN>(a, u);
+    Prefix prefix = {0, 0};
+    if constexpr (SEEN == kPrefix) {
+        const Part part = find_part<kManyRows, kManyStep>(a, rest);
+        t = part.tile;
+        split = part.split;
+        splits = part.splits;
+    } else {
+        const int u = rest % a.many_tiles;
+        split = rest / a.many_tiles;
+        splits = a.splits;
+        if (a.ordered) {
+            t = find_longest<kManyRows>(a, u);
+            if ((SEEN == kOwn || SEEN == kBoth) && t.pairs > 0 && t.request < a.requests) prefix = request_prefix(a, t.request);
+        } else {
+            t = find_tile<kManyRows, SEEN>(a, u, &prefix);
+        }
+    }
     if (t.pairs == 0 || (SEEN != kPrefix && t.request < a.requests && t.request_pairs < kManyPairs)) return;
     if (SEEN == kPrefix && (t.request >= a.n_groups || t.length == 0)) return;
-    const int from = SEEN == kOwn && t.request < a.requests ? request_prefix(a, t.request) : 0;       // the first token that is looked at
+    constexpr bool kBehind = SEEN == kOwn || SEEN == kBoth;
+    const int from = kBehind ? prefix.tokens : 0;        // the request's own tokens begin here
     // positions: of the tile for the steps, of the wavefront for its masks
     const int row0 = t.row0 + t.pair0 / a.group, rest0 = t.pair0 % a.group;       // row and head of the tile's first pair
     auto position_of = [&](int i) { return i < t.pairs ? a.positions[row0 + by_group(a, rest0 + i)] : -1; };
@@ -615,11 +728,15 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     // The blocks of a step: lane l loads the entry of sixteen l % 4, through the vector unit, whose loads end in order (a scalar load on
     // its way would make every wait for the LDS one for all).  It is asked for three steps ahead, the codes two.
     const int32_t *table = a.table + (int64_t)(SEEN == kPrefix ? leader_of(a, t.request) : t.request) * a.width;
-    auto token_of = [&](int step) { return step * kManyStep + lane % 4 * 16; };
-    auto entry_at = [&](int step) { const int token = token_of(step); return table[token < t.length ? token >> a.block_log : 0]; };
+    const int32_t *common_table = a.table + (int64_t)prefix.leader * a.width;
+    auto token_of = [&](int step) { return number_of<SEEN>(step) * kManyStep + lane % 4 * 16; };
+    auto entry_at = [&](int step) {
+        const int token = token_of(step);
+        return (SEEN == kBoth && !(step & kOwnStep) ? common_table : table)[token < end_of<SEEN>(step, from, t.length) ? token >> a.block_log : 0];
+    };
     struct Blocks { int own, here; };                     // of the wavefront's sixteen, -1: none; a bit for each sixteen that has one
     auto blocks_at = [&](int step, int entry) {
-        const bool is = token_of(step) < t.length && (uint32_t)entry < (uint32_t)a.blocks;
+        const bool is = token_of(step) < end_of<SEEN>(step, from, t.length) && (uint32_t)entry < (uint32_t)a.blocks;
         return Blocks{__builtin_amdgcn_readlane(is ? entry : -1, wave), (int)__ballot(is) & 15};
     };
     const KvLayout layout{DIM, 1 << a.block_log};
@@ -628,12 +745,14 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     const uint32_t block_bytes = (uint32_t)a.kv_heads * layout.head_bytes();
     HeldMany<DIM> held;
     auto load = [&](int step, int id) {
-        load_many<DIM>(head_part + (uint64_t)(uint32_t)max(id, 0) * block_bytes, (step * kManyStep + wave * 16) & (layout.tokens - 1), places, held);
+        load_many<DIM>(head_part + (uint64_t)(uint32_t)max(id, 0) * block_bytes, (number_of<SEEN>(step) * kManyStep + wave * 16) & (layout.tokens - 1), places, held);
     };
     // Without a window and splits the first steps are known before the positions are, and with them the first codes: the chain of loads
     // that a tile begins with is then one link shorter.
-    const bool early = !a.window && a.splits == 1;
-    const int held_steps = (t.length + kManyStep - 1) / kManyStep;
+    const bool early = !a.window && splits == 1;
+    Walk<SEEN == kBoth> steps{{(from + kManyStep - 1) / kManyStep, 0, 0, 0},
+                              {t.length > from ? (t.length + kManyStep - 1) / kManyStep - from / kManyStep : 0, 0, from / kManyStep, 0}, 0};
+    steps.sum();
     int step = 0, step_1 = 0, step_2 = 0, entry = 0;      // this step and those after it
     Blocks these = {-1, 0}, next = {-1, 0};               // of this step and the next
     auto begin_at = [&](int s0, int s1, int s2) {
@@ -646,20 +765,22 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
         next = blocks_at(step_1, second);
         load(step, these.own);
     };
-    const int low = from / kManyStep;
-    if (early && t.length > from) begin_at(low, min(low + 1, held_steps - 1), min(low + 2, held_steps - 1));
+    if (early && steps.count > 0) begin_at(steps.at(0), steps.at(min(1, steps.count - 1)), steps.at(min(2, steps.count - 1)));
     const int highest = wave_max(max(p0, p1));
     const int seeing = -wave_max(max(p0 >= 0 ? -p0 : -0x7fffffff, p1 >= 0 ? -p1 : -0x7fffffff));
-    const Steps steps = steps_of<kManyStep>(a, seeing, highest, t.length, from);
-    const int each = max((steps.count + a.splits - 1) / a.splits, SEEN == kAll ? 0 : kFewest / kManyStep), begin = split * each, end = min(steps.count, begin + each);
+    steps.own = steps_of<kManyStep>(a, seeing, highest, t.length, from);
+    if (SEEN == kBoth) steps.common = steps_of<kManyStep>(a, seeing, highest, from, 0);
+    steps.sum();
+    const int each = max((steps.count + splits - 1) / splits, SEEN == kOwn ? kFewest / kManyStep : 0), begin = split * each, end = min(steps.count, begin + each);
     if (split > 0 && begin >= end) return;
-    const bool whole = each >= steps.count && SEEN != kPrefix && from == 0;
+    const bool whole = each >= steps.count && SEEN != kPrefix && (SEEN != kOwn || from == 0);
     auto clamped = [&](int i) { return steps.at(min(i, end - 1)); };       // behind the last step, that one again (see kv_attend)
     if (!early && begin < end) begin_at(steps.at(begin), clamped(begin + 1), clamped(begin + 2));
     const int own = __shfl(wave < 2 ? p0 : p1, wave % 2 * 32 + col);
-    const int position = min(own, t.length - 1), last_sink = a.window ? own - a.window : -1;
+    const int tokens = SEEN == kBoth ? max(t.length, from) : t.length;
+    const int position = min(own, tokens - 1), last_sink = a.window ? own - a.window : -1;
     const int wave_lowest = -wave_max(there ? -max(own, -1) : -0x7fffffff), wave_highest = wave_max(own);
-    const int full_to = min(wave_lowest, t.length - 1), full_from = a.window ? wave_highest - a.window + 1 : 0;
+    const int full_to = min(wave_lowest, tokens - 1), full_from = a.window ? wave_highest - a.window + 1 : 0;
     f32x16_t o[kD];
 #pragma unroll
     for (int d = 0; d < kD; ++d)
@@ -670,14 +791,14 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
 
     // what is not held may be anything: its values are to be finite, its scores are masked
     auto blank = [&](int step, int id) {
-        const int g = lane / 16, h = g % 2, token0 = step * kManyStep + wave * 16;
-        if (id >= 0 && token0 + 16 <= t.length && (SEEN != kOwn || token0 >= from)) return;
+        const int g = lane / 16, h = g % 2, token0 = number_of<SEEN>(step) * kManyStep + wave * 16, least = least_of<SEEN>(step, from), limit = end_of<SEEN>(step, from, t.length);
+        if (id >= 0 && token0 + 16 <= limit && (!kBehind || token0 >= least)) return;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int token = token0 + (h + 2 * k) * 4 + r;
-                const bool is = id >= 0 && token < t.length && (SEEN != kOwn || token >= from);
+                const bool is = id >= 0 && token < limit && (!kBehind || token >= least);
                 held.value_scale[k] &= is ? 0xffffffffu : ~(0xffu << (8 * r));
             }
     };
@@ -721,7 +842,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
     __syncthreads();
     for (int i = begin; i < end; ++i) {
-        const int buffer = (i - begin) & 1, token0 = step * kManyStep;
+        const int buffer = (i - begin) & 1, token0 = number_of<SEEN>(step) * kManyStep, least = least_of<SEEN>(step, from), limit = end_of<SEEN>(step, from, t.length);
         blank(step_1, next.own);
         // scores, and in the shadow of their products the next step's codes into the other buffer
         f32x16_t s[2];
@@ -747,15 +868,16 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
         const int step_3 = clamped(i + 3);
         entry = entry_at(step_3);
         load(step_2, later.own);
-        if (!idle && token0 <= min(wave_highest, t.length - 1)) {
-            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) || (SEEN == kOwn && token0 < from) || these.here != 15) {
+        if (!idle && token0 <= min(wave_highest, limit - 1)) {
+            if (token0 + kManyStep - 1 > full_to || (token0 < full_from && token0 + kManyStep > a.sinks) ||
+                (kBehind && (token0 < least || token0 + kManyStep > limit)) || these.here != 15) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int token = token0 + b * 32 + 8 * (r / 4) + 4 * half + r % 4;
                         const bool seen = (these.here >> (2 * b + r / 8) & 1) && token <= position && (token > last_sink || token < a.sinks) &&
-                                          (SEEN != kOwn || token >= from);
+                                          (!kBehind || (token >= least && token < limit));
                         s[b][r] = seen ? s[b][r] : -INFINITY;
                     }
             }
@@ -806,7 +928,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
     if (!there) return;
     // lane: pair col, values 32 d + 8 (r / 4) + 4 half + r % 4
     const int64_t out_row = (int64_t)row * a.q_heads + qh;
-    float *parts = a.parts + (SEEN == kPrefix || SEEN == kOwn ? out_row * a.slots + a.first_slot + split : out_row * a.splits + split) * (DIM + kPartExtra);
+    float *parts = a.parts + (SEEN == kPrefix ? out_row * a.slots + split : SEEN == kOwn ? out_row * a.slots + a.prefix_splits + split : out_row * a.splits + split) * (DIM + kPartExtra);
     const float inverse = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
     for (int d = 0; d < kD; ++d)
@@ -822,11 +944,38 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
                 *reinterpret_cast<f32x4_t *>(parts + at) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
             }
         }
-    if ((a.splits > 1 || SEEN == kPrefix || SEEN == kOwn) && half == 0) {
+    if ((splits > 1 || SEEN == kPrefix || SEEN == kOwn) && half == 0) {
         parts[DIM] = base;
         parts[DIM + 1] = sum;
         parts[DIM + 2] = __builtin_bit_cast(float, whole || steps.count == 0 ? 1 : (steps.count + each - 1) / each);
         parts[DIM + 3] = __builtin_bit_cast(float, (int)(from > 0));
+    }
+}
+
+template <int DT, int DIM, int SEEN>
+__global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_attend_many(AttendArgs a) {
+    __shared__ ManyKeys<DIM> keys;
+    __shared__ ManyValues<DIM> values;
+    attend_many_rows<DT, DIM, SEEN>(a, blockIdx.x, keys, values);
+}
+
+// Prefixes and what requests have behind them in one launch: the workgroups of prefixes first, which take longest; while they keep the matrix cores busy, the
+// others read.  MANY: prefixes by 128 pairs.
+template <int DT, int DIM, bool MANY>
+__global__ __launch_bounds__(256, MANY ? (DIM == 256 ? 1 : DIM == 128 ? 2 : 3) : DIM == 256 ? 2 : 4) void kv_attend_shared(AttendArgs a) {
+    __shared__ union Lds {
+        __device__ Lds() {}
+        struct { FewJoin<DIM> join; FewSums base, sum; } few;
+        struct { ManyKeys<MANY ? DIM : 32> keys; ManyValues<MANY ? DIM : 32> values; } many;
+    } lds;
+    const int group = blockIdx.x;
+    if constexpr (MANY) {
+        if (group < a.prefix_groups) attend_many_rows<DT, DIM, kPrefix>(a, group, lds.many.keys, lds.many.values);
+        else if (group < a.prefix_groups + a.own_many) attend_many_rows<DT, DIM, kOwn>(a, group - a.prefix_groups, lds.many.keys, lds.many.values);
+        else attend_few<DT, DIM, kOwn>(a, group - a.prefix_groups - a.own_many, lds.few.join, lds.few.base, lds.few.sum);
+    } else {
+        if (group < a.prefix_groups) attend_few<DT, DIM, kPrefix>(a, group, lds.few.join, lds.few.base, lds.few.sum);
+        else attend_few<DT, DIM, kOwn>(a, group - a.prefix_groups, lds.few.join, lds.few.base, lds.few.sum);
     }
 }
 
@@ -877,7 +1026,7 @@ __global__ __launch_bounds__(256) void kv_attend_join(AttendArgs a) {
     *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + (int64_t)blockIdx.x * DIM + 4 * at) = y;
 }
 
-// Joins what the prefix's splits (the first a.first_slot slots of a row and query head) and its own (those behind) gave, as kv_attend_join.
+// Joins what the prefix's splits (the first a.prefix_splits slots of a row and query head) and its own (those behind) gave, as kv_attend_join.
 template <int DT, int DIM>
 __global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
     typedef typename Elem<DT>::type T;
@@ -885,14 +1034,14 @@ __global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
     __shared__ float factor[256], bases[4], sums[4];
     __shared__ f32x4_t part[kGroups][kLanes];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const float *p = a.parts + (int64_t)blockIdx.x * a.slots * (DIM + kPartExtra), *own = p + a.first_slot * (DIM + kPartExtra);
+    const float *p = a.parts + (int64_t)blockIdx.x * a.slots * (DIM + kPartExtra), *own = p + a.prefix_splits * (DIM + kPartExtra);
     const bool slot = tid < a.slots;
     const float own_base = slot ? p[tid * (DIM + kPartExtra) + DIM] : 0.f, own_sum = slot ? p[tid * (DIM + kPartExtra) + DIM + 1] : 0.f;
     // (what is read of results that there are not is not used: a row that starts leave out may have any numbers)
     const int own_count = max(min(__builtin_bit_cast(int, own[DIM + 2]), a.splits), 0);
-    const int count = __builtin_bit_cast(int, own[DIM + 3]) != 0 ? max(min(__builtin_bit_cast(int, p[DIM + 2]), a.first_slot), 0) : 0;
+    const int count = __builtin_bit_cast(int, own[DIM + 3]) != 0 ? max(min(__builtin_bit_cast(int, p[DIM + 2]), a.prefix_splits), 0) : 0;
     if (count + own_count <= 1 && count == 0) return;
-    const bool mine = tid < count || (tid >= a.first_slot && tid - a.first_slot < own_count);
+    const bool mine = tid < count || (tid >= a.prefix_splits && tid - a.prefix_splits < own_count);
     const float base = mine ? own_base : -3.4028234663852886e38f;
     float m = base;
     for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
@@ -910,7 +1059,7 @@ __global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
     f32x4_t v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int i = group; i < count + own_count; i += kGroups) {
-        const int s = i < count ? i : a.first_slot + i - count;
+        const int s = i < count ? i : a.prefix_splits + i - count;
         v += *reinterpret_cast<const f32x4_t *>(p + s * (DIM + kPartExtra) + 4 * at) * factor[s];
     }
     part[group][at] = v;
@@ -963,89 +1112,110 @@ size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, i
     return s == 1 ? 0 : (size_t)rows * d.q_heads * s * (d.head_dim + kPartExtra) * 4;
 }
 
-template <int DT, int DIM> static hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t st) {
+template <int DT, int DIM, int SEEN> static hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t st) {
     if (a.many) {
-        kv_attend_many<DT, DIM, kAll><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
+        kv_attend_many<DT, DIM, SEEN><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.tiles) kv_attend<DT, DIM, kAll><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
+    if (a.tiles) kv_attend<DT, DIM, SEEN><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 template <int DT> static hipError_t launch_attend_type(const AttendArgs &a, int dim, hipStream_t st) {
-    return dim == 64 ? launch_attend_dim<DT, 64>(a, st) : dim == 128 ? launch_attend_dim<DT, 128>(a, st) : launch_attend_dim<DT, 256>(a, st);
+    return dim == 64 ? launch_attend_dim<DT, 64, kAll>(a, st) : dim == 128 ? launch_attend_dim<DT, 128, kAll>(a, st) : launch_attend_dim<DT, 256, kAll>(a, st);
 }
 
-hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
+static AttendArgs with_sizes(const nnv_attention_desc &d, const AttendArgs &args) {
     AttendArgs a = args;
     a.many = attend_many(d, a.requests, a.rows);
     a.tiles = a.many ? 2 * a.requests : attend_tiles(a.requests, a.rows, a.group, kTileRows);
     a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
     a.splits = attend_splits(d, a.requests, a.rows);
-    a.parts = static_cast<float *>(ws);
     a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
     // the order costs a loop over the requests, and is for tiles that take many steps
     a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
+    return a;
+}
+
+hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
+    AttendArgs a = with_sizes(d, args);
+    a.parts = static_cast<float *>(ws);
     return d.dtype == NNV_F16 ? launch_attend_type<NNV_F16>(a, d.head_dim, st) : launch_attend_type<NNV_BF16>(a, d.head_dim, st);
 }
 
 // ---- a prefix read once for the requests that share it, and what each has behind it ------------------------------------------
 
-// Both are the kernels above; their partial results are joined by one that knows of both.  The prefix goes to kv_attend_many, which converts its codes once for
-// 128 pairs, where a group has that many on average as fill a wavefront of it.
-static bool prefix_many(const nnv_attention_desc &d, int rows, int groups) { return (int64_t)rows * (d.q_heads / d.kv_heads) >= (int64_t)kManyPairs * groups; }
+// Where requests have 256 pairs and more on average, their tiles go over the prefix by themselves: it is converted for 128 pairs at a time either way, and nothing is to
+// be joined (16 requests of up to 256 rows behind 4096 tokens, 32 heads: ... us, in two parts 328).
+static bool shared_by_request(const nnv_attention_desc &d, int requests, int rows) { return (int64_t)rows * (d.q_heads / d.kv_heads) >= (int64_t)2 * kManyRows * requests; }
 
-struct SharedSplits { int prefix, own; };
-static SharedSplits shared_splits(const nnv_attention_desc &d, int requests, int rows, int groups) {
-    const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens, each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
-    const int64_t pairs = (int64_t)rows * (d.q_heads / d.kv_heads);
-    const int64_t most = (capacity + kFewest - 1) / kFewest < kMostSplits ? (capacity + kFewest - 1) / kFewest : kMostSplits;
-    auto cut = [&](int64_t tiles, int64_t fill) {
-        int64_t s = (fill + tiles * d.kv_heads - 1) / (tiles * d.kv_heads);
-        s = s < most ? s : most;
-        while (s > 1 && (s * each > (int64_t)128 << 20 || s * kv_attention_groups(d, requests > groups ? requests : groups, rows) >= 1 << 24)) s = s / 2;
-        return (int)(s < 1 ? 1 : s);
+// Otherwise prefixes and what is behind them are two parts, whose results are joined.  The prefix goes by 128 pairs, converted once for them, where a group has as
+// many on average as fill a wavefront's part of those.
+struct SharedSizes { bool many; int units, least, prefix, own, slots; int64_t prefix_groups, own_many, own_few; };
+static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    const int group = d.q_heads / d.kv_heads;
+    const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens, pairs = (int64_t)rows * group, each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
+    const bool own_many = attend_many(d, requests, rows);
+    SharedSizes s{};
+    s.many = own_many || pairs >= (int64_t)kManyPairs * groups;
+    auto within = [&](int64_t splits, int64_t most) {     // of memory, and of what the join takes
+        splits = splits < most ? splits : most;
+        splits = splits < kMostSplits ? splits : kMostSplits;
+        while (splits > 1 && splits * each > (int64_t)128 << 20) splits = splits / 2;
+        return (int)(splits < 1 ? 1 : splits);
     };
-    const int64_t tile = prefix_many(d, rows, groups) ? kManyRows : kTileRows, full = pairs / tile, least = groups < rows ? groups : rows;
-    const int64_t own = pairs / (attend_many(d, requests, rows) ? kManyRows : kTileRows), least_own = requests < rows ? requests : rows;
-    return {groups ? cut(full > least ? full : least, 512) : 0, cut(own > least_own ? own : least_own > 0 ? least_own : 1, 1024)};
+    const int64_t tile = s.many ? kManyRows : kTileRows, prefix_tiles = pairs / tile + groups + 1;
+    if (groups) {
+        const int64_t target = s.many ? 256 : 512;
+        s.units = (int)((target + d.kv_heads - 1) / d.kv_heads);
+        s.least = s.many ? 4 : 4;
+        if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
+        else s.prefix = within(s.units, capacity / 128 + 1);
+        s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : s.units + prefix_tiles) * d.kv_heads;
+    }
+    const int64_t own_tile = own_many ? kManyRows : kTileRows, full = pairs / own_tile, least = requests < rows ? requests : rows;
+    const int64_t own_tiles = (full > least ? full : least > 0 ? least : 1) * d.kv_heads;
+    s.own = within((1024 + own_tiles - 1) / own_tiles, capacity / kFewest + 1);
+    auto own_groups = [&] {
+        s.own_many = own_many ? (int64_t)attend_tiles(requests, rows, group, kManyRows) * d.kv_heads * s.own : 0;
+        s.own_few = (own_many ? 2 * (int64_t)requests : attend_tiles(requests, rows, group, kTileRows)) * d.kv_heads * s.own;
+        return s.own_many + s.own_few;
+    };
+    while (own_groups() + s.prefix_groups >= 1 << 24 && s.own > 1) s.own /= 2;
+    if (own_groups() + s.prefix_groups >= 1 << 24 && groups > 64 && s.prefix > 1) s.prefix = 1, s.prefix_groups = prefix_tiles * d.kv_heads;
+    s.slots = s.prefix + s.own;
+    return s;
+}
+
+int64_t kv_attention_shared_groups(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    if (shared_by_request(d, requests, rows)) return kv_attention_groups(d, requests, rows);
+    const SharedSizes s = shared_sizes(d, requests, rows, groups);
+    return s.prefix_groups + s.own_many + s.own_few;
 }
 
 size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups) {
-    const SharedSplits s = shared_splits(d, requests, rows, groups);
-    return (size_t)rows * d.q_heads * (s.prefix + s.own) * (d.head_dim + kPartExtra) * 4;
+    if (shared_by_request(d, requests, rows)) return kv_attention_workspace_bytes(d, requests, rows);
+    return (size_t)rows * d.q_heads * shared_sizes(d, requests, rows, groups).slots * (d.head_dim + kPartExtra) * 4;
 }
 
 template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attention_desc &d, const AttendArgs &args, hipStream_t st) {
-    AttendArgs a = args;
-    const SharedSplits s = shared_splits(d, a.requests, a.rows, a.n_groups);
-    a.slots = s.prefix + s.own;
-    if (a.n_groups) {
-        AttendArgs p = a;
-        p.splits = s.prefix;
-        p.first_slot = 0;
-        p.many = p.ordered = 0;
-        p.many_tiles = attend_tiles(a.n_groups, a.rows, a.group, kManyRows);
-        p.tiles = attend_tiles(a.n_groups, a.rows, a.group, kTileRows);
-        if (prefix_many(d, a.rows, a.n_groups)) kv_attend_many<DT, DIM, kPrefix><<<(unsigned)(p.many_tiles * p.kv_heads * p.splits), 256, 0, st>>>(p);
-        else kv_attend<DT, DIM, kPrefix><<<(unsigned)(p.tiles * p.kv_heads * p.splits), 64 * kAttendWaves, 0, st>>>(p);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    a.first_slot = s.prefix;
+    AttendArgs a = with_sizes(d, args);
+    if (shared_by_request(d, a.requests, a.rows)) return launch_attend_dim<DT, DIM, kBoth>(a, st);
+    const SharedSizes s = shared_sizes(d, a.requests, a.rows, a.n_groups);
+    a.slots = s.slots;
+    a.prefix_splits = s.prefix;
+    a.prefix_units = s.units;
+    a.prefix_least = s.least;
+    a.prefix_groups = (int)s.prefix_groups;
+    a.own_many = (int)s.own_many;
     a.splits = s.own;
-    a.many = attend_many(d, a.requests, a.rows);
-    a.tiles = a.many ? 2 * a.requests : attend_tiles(a.requests, a.rows, a.group, kTileRows);
-    a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
-    a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
-    if (a.many) kv_attend_many<DT, DIM, kOwn><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (a.tiles) kv_attend<DT, DIM, kOwn><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
-    e = hipGetLastError();
+    const unsigned groups = (unsigned)(s.prefix_groups + s.own_many + s.own_few);
+    if (s.many) kv_attend_shared<DT, DIM, true><<<groups, 256, 0, st>>>(a);
+    else kv_attend_shared<DT, DIM, false><<<groups, 256, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     kv_attend_join_shared<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
     return hipGetLastError();
@@ -1057,7 +1227,6 @@ template <int DT> static hipError_t launch_shared_type(const nnv_attention_desc 
 hipError_t launch_kv_attention_shared(const nnv_attention_desc &d, const AttendArgs &args, void *ws, hipStream_t st) {
     AttendArgs a = args;
     a.parts = static_cast<float *>(ws);
-    a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
     return d.dtype == NNV_F16 ? launch_shared_type<NNV_F16>(d, a, st) : launch_shared_type<NNV_BF16>(d, a, st);
 }
 

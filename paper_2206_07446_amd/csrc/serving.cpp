@@ -322,9 +322,9 @@ int nnv_kv_attention_blocks(const nnv_attention_desc *desc, int n_requests, int 
 
 size_t nnv_kv_attention_shared_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups) {
     if (check_attention(desc) || check_counts(n_requests, n_rows) || n_rows == 0 || n_groups < 0 || n_groups > kMostRequests ||
-        kv_attention_groups(*desc, std::max(n_requests, n_groups), n_rows) > kMostGroups)
+        kv_attention_shared_groups(*desc, n_requests, n_rows, n_requests ? n_groups : 0) > kMostGroups)
         return 0;
-    return kv_attention_shared_workspace_bytes(*desc, n_requests, n_rows, n_groups);
+    return kv_attention_shared_workspace_bytes(*desc, n_requests, n_rows, n_requests ? n_groups : 0);
 }
 
 int nnv_kv_attention_shared(const nnv_attention_desc *desc, int n_requests, int n_rows, int n_groups, const void *q, const int32_t *block_table,
@@ -334,16 +334,17 @@ int nnv_kv_attention_shared(const nnv_attention_desc *desc, int n_requests, int 
     if (const int rc = check_counts(n_requests, n_rows)) return rc;
     if (n_groups < 0 || n_groups > kMostRequests) return NNV_E_ARG;
     if (n_rows == 0) return NNV_OK;
-    if (kv_attention_groups(*desc, std::max(n_requests, n_groups), n_rows) > kMostGroups) return NNV_E_ARG;
+    if (kv_attention_shared_groups(*desc, n_requests, n_rows, n_requests ? n_groups : 0) > kMostGroups) return NNV_E_ARG;
     if (n_groups && (!groups || !shared)) return NNV_E_NULL;
     if (off4(groups) || off4(shared)) return NNV_E_ALIGN;
+    if (!n_requests) n_groups = 0;
     const size_t need = kv_attention_shared_workspace_bytes(*desc, n_requests, n_rows, n_groups);
     AttendArgs a;
     if (const int rc = attend_args(desc, n_requests, n_rows, q, block_table, starts, lengths, positions, cache, out, workspace, workspace_bytes, need, a)) return rc;
     const size_t g = n_groups;
     for (const Bytes &in : {Bytes(groups, g ? 4 * (g + 1) : 0), Bytes(shared, 4 * g)})
         if (in.meets({out, (size_t)2 * n_rows * desc->q_heads * desc->head_dim}) || in.meets({workspace, need})) return NNV_E_ARG;
-    a.groups = groups; a.shared = shared; a.n_groups = n_requests ? n_groups : 0;
+    a.groups = groups; a.shared = shared; a.n_groups = n_groups;
     return finish(launch_kv_attention_shared(*desc, a, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 

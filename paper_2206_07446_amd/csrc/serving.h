@@ -64,11 +64,14 @@ struct AttendArgs {
     int flip;           // sign bits of a pair of 16-bit values where the factor is negative
     const int32_t *groups, *shared, *selected;
     int n_groups, keep;
-    int slots, first_slot;                     // partial results of a row and query head, and the first of this launch's (nnv_kv_attention_shared)
+    // nnv_kv_attention_shared: partial results of a row and query head, the most splits of a prefix (their results come first), workgroups that prefixes are cut into (of a
+    // key head) and the fewest steps of one, launched workgroups of prefixes and of requests of many rows
+    int slots, prefix_splits, prefix_units, prefix_least, prefix_groups, own_many;
 };
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows);     // tiles of rows times key/value heads
 size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, int rows);
 hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &a, void *ws, hipStream_t st);
+int64_t kv_attention_shared_groups(const nnv_attention_desc &d, int requests, int rows, int groups);
 size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups);
 hipError_t launch_kv_attention_shared(const nnv_attention_desc &d, const AttendArgs &a, void *ws, hipStream_t st);
 int64_t kv_attention_blocks_groups(const nnv_attention_desc &d, int rows);
