@@ -199,10 +199,14 @@ template <int R, int S> __device__ static inline Part find_part(const AttendArgs
     const bool mine = lane < a.n_groups;
     const int start = mine ? start_of<kPrefix>(a, lane) : 0, end = mine ? start_of<kPrefix>(a, lane + 1) : 0, tokens = mine ? prefix_of(a, lane) : 0;
     const int tiles = (int)((max((int64_t)(end - start) * a.group, (int64_t)0) + R - 1) / R), steps = (tokens + S - 1) / S;
-    float total = (float)tiles * (float)steps;
-    for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
-    // (rounded up by more than the sum is off: no more parts than there are workgroups)
-    const int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / a.prefix_units), 1e9f));
+    float total = (float)tiles * (float)steps, whole = (float)tiles;
+    for (int s = 1; s < 64; s *= 2) {
+        total += __shfl_xor(total, s);
+        whole += __shfl_xor(whole, s);
+    }
+    // (each tile's last part counts as one more; rounded up by more than the sum is off: no more parts than there are workgroups)
+    const float units = fmaxf(a.prefix_units - whole, 0.5f * a.prefix_units);
+    const int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / units), 1e9f));
     const int splits = min((steps + each - 1) / each, a.prefix_splits), parts = tiles * splits;
     int before = 0, sum = parts;
     for (int s = 1; s < 64; s *= 2) {
@@ -407,6 +411,7 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(co
             t = find_row<kTileRows>(a, u / each, u % each * kTileRows);
         } else if (a.many) {
             t = tile_of<kTileRows>(a, u / 2, clamped_start(a, a.starts[u / 2]), clamped_start(a, a.starts[u / 2 + 1]), a.lengths[u / 2], u % 2);
+            if (t.pairs == 0 || t.request_pairs >= kManyPairs) return;
             if (SEEN == kOwn || SEEN == kBoth) prefix = request_prefix(a, u / 2);
         } else {
             t = find_tile<kTileRows, SEEN>(a, u, &prefix);
@@ -703,7 +708,10 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_many_r
         splits = a.splits;
         if (a.ordered) {
             t = find_longest<kManyRows>(a, u);
-            if ((SEEN == kOwn || SEEN == kBoth) && t.pairs > 0 && t.request < a.requests) prefix = request_prefix(a, t.request);
+            if ((SEEN == kOwn || SEEN == kBoth) && t.pairs > 0 && t.request < a.requests) {
+                if (t.request_pairs < kManyPairs) return;
+                prefix = request_prefix(a, t.request);
+            }
         } else {
             t = find_tile<kManyRows, SEEN>(a, u, &prefix);
         }
@@ -1073,6 +1081,64 @@ __global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
     *reinterpret_cast<ElemVec<DT, 4> *>(static_cast<T *>(a.out) + (int64_t)blockIdx.x * DIM + 4 * at) = y;
 }
 
+// The same with a wavefront to a row and query head, where there are many of these: nothing waits for another, and a wavefront's loads are all on their way.
+template <int DT, int DIM>
+__global__ __launch_bounds__(256) void kv_attend_join_rows(AttendArgs a, int all) {
+    typedef typename Elem<DT>::type T;
+    constexpr int kEach = DIM / 64;
+    typedef float FV __attribute__((ext_vector_type(kEach)));
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    if (row >= all) return;
+    const float *p = a.parts + (int64_t)row * a.slots * (DIM + kPartExtra), *own = p + a.prefix_splits * (DIM + kPartExtra);
+    // (a lane to a slot, and one more slot each where there are more than 64; what is read of results that there are not is not used)
+    float bases[4], sums[4], m = -3.4028234663852886e38f, l = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i * 64 < a.slots) {
+            const int s = min(i * 64 + lane, a.slots - 1);
+            bases[i] = p[s * (DIM + kPartExtra) + DIM];
+            sums[i] = p[s * (DIM + kPartExtra) + DIM + 1];
+        }
+    const int own_count = uniform(max(min(__builtin_bit_cast(int, own[DIM + 2]), a.splits), 0));
+    const int count = __builtin_bit_cast(int, own[DIM + 3]) != 0 ? uniform(max(min(__builtin_bit_cast(int, p[DIM + 2]), a.prefix_splits), 0)) : 0;
+    if (count == 0 && own_count <= 1) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i * 64 < a.slots) {
+            const int s = i * 64 + lane;
+            if (s < count || (s >= a.prefix_splits && s - a.prefix_splits < own_count)) m = fmaxf(m, bases[i]);
+        }
+    for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i * 64 < a.slots) {
+            const int s = i * 64 + lane;
+            const bool mine = s < count || (s >= a.prefix_splits && s - a.prefix_splits < own_count);
+            bases[i] = mine ? __builtin_amdgcn_exp2f(bases[i] - m) : 0.f;
+            l += mine ? sums[i] * bases[i] : 0.f;
+        }
+    for (int s = 1; s < 64; s *= 2) l += __shfl_xor(l, s);
+    FV v = {};
+    const int all_parts = count + own_count;
+    for (int i0 = 0; i0 < all_parts; i0 += 8) {           // (behind the last that one again, which counts for nothing)
+        FV x[8];
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = min(i0 + k, all_parts - 1), s = i < count ? i : a.prefix_splits + i - count, at = s >> 6;
+            const float factor = at == 0 ? bases[0] : at == 1 ? bases[1] : at == 2 ? bases[2] : bases[3];
+            x[k] = *reinterpret_cast<const FV *>(p + s * (DIM + kPartExtra) + kEach * lane);
+            f[k] = i0 + k < all_parts ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, factor), s & 63)) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += x[k] * f[k];
+    }
+    ElemVec<DT, kEach> y;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) y[i] = (T)(l == 0 ? 0.f : v[i] / l);
+    *reinterpret_cast<ElemVec<DT, kEach> *>(static_cast<T *>(a.out) + (int64_t)row * DIM + kEach * lane) = y;
+}
+
 static int attend_tiles(int requests, int rows, int group, int tile) { return (int)(((int64_t)rows * group) / tile) + requests + 1; }
 
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows) {
@@ -1158,7 +1224,7 @@ struct SharedSizes { bool many; int units, least, prefix, own, slots; int64_t pr
 static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int rows, int groups) {
     const int group = d.q_heads / d.kv_heads;
     const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens, pairs = (int64_t)rows * group, each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
-    const bool own_many = attend_many(d, requests, rows);
+    const bool own_many = attend_many(d, requests, rows) && pairs >= (int64_t)kManyPairs * requests;      // (of fewer on average, nearly all are few)
     SharedSizes s{};
     s.many = own_many || pairs >= (int64_t)kManyPairs * groups;
     auto within = [&](int64_t splits, int64_t most) {     // of memory, and of what the join takes
@@ -1169,16 +1235,16 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
     };
     const int64_t tile = s.many ? kManyRows : kTileRows, prefix_tiles = pairs / tile + groups + 1;
     if (groups) {
-        const int64_t target = s.many ? 256 : 512;
+        const int64_t target = 512;
         s.units = (int)((target + d.kv_heads - 1) / d.kv_heads);
-        s.least = s.many ? 4 : 4;
+        s.least = s.many ? 8 : 4;
         if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
         else s.prefix = within(s.units, capacity / 128 + 1);
         s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : s.units + prefix_tiles) * d.kv_heads;
     }
     const int64_t own_tile = own_many ? kManyRows : kTileRows, full = pairs / own_tile, least = requests < rows ? requests : rows;
     const int64_t own_tiles = (full > least ? full : least > 0 ? least : 1) * d.kv_heads;
-    s.own = within((1024 + own_tiles - 1) / own_tiles, capacity / kFewest + 1);
+    s.own = within((512 + own_tiles - 1) / own_tiles, capacity / kFewest + 1);
     auto own_groups = [&] {
         s.own_many = own_many ? (int64_t)attend_tiles(requests, rows, group, kManyRows) * d.kv_heads * s.own : 0;
         s.own_few = (own_many ? 2 * (int64_t)requests : attend_tiles(requests, rows, group, kTileRows)) * d.kv_heads * s.own;
@@ -1211,13 +1277,17 @@ template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attenti
     a.prefix_least = s.least;
     a.prefix_groups = (int)s.prefix_groups;
     a.own_many = (int)s.own_many;
+    a.many = s.own_many > 0;
+    a.tiles = (int)(s.own_few / ((int64_t)a.kv_heads * s.own));
     a.splits = s.own;
     const unsigned groups = (unsigned)(s.prefix_groups + s.own_many + s.own_few);
     if (s.many) kv_attend_shared<DT, DIM, true><<<groups, 256, 0, st>>>(a);
     else kv_attend_shared<DT, DIM, false><<<groups, 256, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    kv_attend_join_shared<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
+    const int all = a.rows * a.q_heads;
+    if (all >= 4096) kv_attend_join_rows<DT, DIM><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, all);
+    else kv_attend_join_shared<DT, DIM><<<(unsigned)all, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 template <int DT> static hipError_t launch_shared_type(const nnv_attention_desc &d, const AttendArgs &a, hipStream_t st) {

@@ -130,6 +130,7 @@ hipError_t launch_kv_bounds(const BoundsArgs &a, int dim, hipStream_t st) {
 
 // ---- selection ----------------------------------------------------------------------------------
 
+typedef double f64x2_t __attribute__((ext_vector_type(2)));
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
 // Numbers in the order of 64-bit keys; a NaN counts as -infinity.  Key 0 is no block's.
@@ -140,113 +141,162 @@ __device__ static inline uint64_t key_of(double v) {
 }
 
 // Scores of a tile of whole rows with a head's blocks: max(q hi, q lo) is max(q, 0) hi + min(q, 0) lo, so that a score is one product over 2 DIM, on the
-// matrix cores in float64: 16 blocks x 4 values x 4 (one 4x4x4 instruction for each four blocks) or 16 query heads (16x16x4).  Lane l holds of block, and of query
-// head, l % 16 (l % 4) the eight values from 32 s + 8 (l / 16): products sum over values in any order.
+// matrix cores in float64: 16 blocks x 4 values x 4 query heads (4x4x4, four of them in an instruction) or x 16 (16x16x4).  Lane l holds of block, and of query
+// head, l % 16 (l % 4) the eight values from 32 s + 8 (l / 16): products sum over values in any order.  Queries lie in the LDS as they enter, the same for all
+// wavefronts; the bounds of a wavefront's next 16 blocks are on their way while it computes.
 template <int DT, int DIM, int COLS>
-__global__ __launch_bounds__(256) void kv_scores(SelectArgs a) {
+__global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_scores(SelectArgs a) {
     typedef typename Elem<DT>::type T;
     constexpr int kSteps = DIM / 32;
-    typedef ElemVec<DT, 8> Q8;
+    __shared__ f64x2_t queries[DIM / 4][4][COLS];                    // max(q, 0) and min(q, 0) of value 32 s + 8 g + e at [8 s + e][g]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % COLS;
-    const int chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks, head = rest % a.kv_heads, u = rest / a.kv_heads;
+    // (chunks last: workgroups go to the chip's eight parts in turn, and of two chunks the second, which fewer requests reach, would keep half of them idle)
+    const int tiles = gridDim.x / (a.kv_heads * a.chunks), head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % tiles, chunk = rest / tiles;
     auto start_of = [&](int i) { return min(max(a.starts[i], a.row0), a.row0 + a.rows); };
-    const Found f = last_place(a.requests, u, a.lengths, start_of, [&](int i, int start) { return (int64_t)((start - a.row0) / a.tile_rows) + i; });
-    const int request = f.request, start = f.start, end = f.end, local = u - ((start - a.row0) / a.tile_rows + request);
-    const int tile0 = start + local * a.tile_rows, rows = min(end - tile0, a.tile_rows);
+    // a row at a time is found by itself; tiles of several begin at floor((starts[i] - row0) / tile_rows) + i
+    const bool single = a.tile_rows == 1;
+    const Found f = last_place(a.requests, single ? a.row0 + u : u, a.lengths, start_of,
+                               [&](int i, int start) { return single ? (int64_t)start : (int64_t)((start - a.row0) / a.tile_rows) + i; });
+    const int local = single ? a.row0 + u - f.start : u - ((f.start - a.row0) / a.tile_rows + f.request);
+    const int tile0 = f.start + local * a.tile_rows, rows = min(f.end - tile0, a.tile_rows);
     if (local < 0 || rows <= 0) return;
     const int length = min(max(f.length, 0), a.width << a.block_log);
-    int last = -1;                                                   // last token that a row of the tile sees
-    for (int r = 0; r < rows; ++r) last = max(last, min(a.positions[tile0 + r], length - 1));
-    const int first_block = chunk * a.chunk_blocks, end_block = min(first_block + a.chunk_blocks, last < 0 ? 0 : (last >> a.block_log) + 1);
-    if (first_block >= end_block) return;
-    const int32_t *table = a.table + (int64_t)request * a.width;
+    int last = lane < rows ? min(a.positions[tile0 + lane], length - 1) : -1;            // the last token that a row sees (16 rows at most)
+    // the first bounds do not wait for the positions: up to these, blocks of the request are read
+    const int first_block = chunk * a.chunk_blocks, held_end = min(first_block + a.chunk_blocks, (length + (1 << a.block_log) - 1) >> a.block_log);
+    if (first_block >= held_end) return;
+    const int32_t *table = a.table + (int64_t)f.request * a.width;
 
-    auto load = [&](int b0, i32x4_t (&hi)[kSteps], i32x4_t (&lo)[kSteps]) {
-        const int b = b0 + lane % 16, id = b < end_block ? table[b] : -1;
-        const bool is = id >= 0 && id < a.blocks;
-        const __bf16 *p = a.bounds + ((int64_t)(is ? id : 0) * a.kv_heads + head) * 2 * DIM + g * 8;
+    struct Bounds { i32x4_t hi[kSteps], lo[kSteps]; bool is; };
+    auto id_of = [&](int b0) { return table[min(b0 + lane % 16, held_end - 1)]; };
+    auto load = [&](int b0, int id, Bounds &b) {
+        b.is = b0 + lane % 16 < held_end && id >= 0 && id < a.blocks;
+        const __bf16 *p = a.bounds + ((int64_t)(b.is ? id : 0) * a.kv_heads + head) * 2 * DIM + g * 8;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            hi[s] = *reinterpret_cast<const i32x4_t *>(p + s * 32);
-            lo[s] = *reinterpret_cast<const i32x4_t *>(p + DIM + s * 32);
+            b.hi[s] = *reinterpret_cast<const i32x4_t *>(p + s * 32);
+            b.lo[s] = *reinterpret_cast<const i32x4_t *>(p + DIM + s * 32);
         }
-        return is;
     };
-    const int many = a.group <= COLS ? 1 : (a.group + COLS - 1) / COLS;      // products of a row's heads
-    const int window = min(a.group, COLS);                                    // columns of a row
-    for (int b0 = first_block + wave * 16; b0 < end_block; b0 += 64) {
-        i32x4_t hi[kSteps], lo[kSteps];
-        const bool is = load(b0, hi, lo);
-        f64x4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        for (int c = 0; c < many; ++c) {
-            const int pair = c * COLS + col, row = many == 1 ? pair / a.group : 0, h = many == 1 ? pair % a.group : pair;
-            const bool there = row < rows && h < a.group;
-            f64x4_t sum = {0, 0, 0, 0};
-            const T *q = static_cast<const T *>(a.q) + ((int64_t)(tile0 + (there ? row : 0)) * a.q_heads + head * a.group + (there ? h : 0)) * DIM + g * 8;
+    const int begin = first_block + wave * 16, window = min(a.group, COLS);      // columns of a row
+    const bool wide = a.group > COLS;                     // a row's heads in several products
+    Bounds first, second;
+    int id_next = 0;
+    if (begin < held_end) {
+        load(begin, id_of(begin), first);
+        id_next = id_of(min(begin + 64, held_end - 1));
+    }
+    for (int s = 1; s < 16; s *= 2) last = max(last, __shfl_xor(last, s));
+    last = __builtin_amdgcn_readfirstlane(last);
+    const int end_block = min(held_end, last < 0 ? 0 : (last >> a.block_log) + 1);
+    if (first_block >= end_block) return;
+    for (int c = 0; c * COLS < (wide ? a.group : 1); ++c) {
+        if (c) {
+            __syncthreads();
+            if (begin < end_block) {
+                load(begin, id_of(begin), first);
+                id_next = id_of(min(begin + 64, held_end - 1));
+            }
+        }
+        // (eight values a thread, neighbours to one place after the other)
+        for (int i = threadIdx.x; i < COLS * 4 * kSteps; i += 256) {
+            const int at = i % COLS, part = i / COLS % 4, s = i / (COLS * 4), pair = c * COLS + at, row = wide ? 0 : at / a.group, h = wide ? pair : at % a.group;
+            ElemVec<DT, 8> q = {};
+            if (row < rows && h < a.group)
+                q = *reinterpret_cast<const ElemVec<DT, 8> *>(static_cast<const T *>(a.q) + ((int64_t)(tile0 + row) * a.q_heads + head * a.group + h) * DIM + s * 32 + part * 8);
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const Q8 q8 = *reinterpret_cast<const Q8 *>(q + s * 32);
+            for (int e = 0; e < 8; ++e) {
+                const float v = a.flip ? -(float)q[e] : (float)q[e];
+                queries[8 * s + e][part][at] = f64x2_t{(double)fmaxf(v, 0.f), (double)fminf(v, 0.f)};
+            }
+        }
+        __syncthreads();
+        const int pair = c * COLS + col, row = wide ? 0 : col / a.group;
+        const bool there = wide ? pair < a.group : row < rows;
+        auto round = [&](int b0, const Bounds &now, Bounds &next) {
+            const int after = min(b0 + 64, held_end - 1);            // (behind the last block, that one again)
+            load(after, id_next, next);
+            id_next = id_of(min(after + 64, held_end - 1));
+            asm volatile("" ::: "memory");             // queries are read again each round: kept, they would take the registers of another wavefront
+            f64x4_t sum = {0, 0, 0, 0}, more = {0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const uint32_t wh = hi[s][e / 2], wl = lo[s][e / 2];
+                    const uint32_t wh = now.hi[s][e / 2], wl = now.lo[s][e / 2];
                     const double x = (double)__builtin_bit_cast(float, e % 2 ? wh & 0xffff0000u : wh << 16);
                     const double y = (double)__builtin_bit_cast(float, e % 2 ? wl & 0xffff0000u : wl << 16);
-                    const float f = a.flip ? -(float)q8[e] : (float)q8[e];
-                    const double up = (double)fmaxf(f, 0.f), down = (double)fminf(f, 0.f);
+                    const f64x2_t q = queries[8 * s + e][g][col];
                     if constexpr (COLS == 4) {
-                        sum[0] = __builtin_amdgcn_mfma_f64_4x4x4f64(x, up, sum[0], 0, 0, 0);
-                        sum[0] = __builtin_amdgcn_mfma_f64_4x4x4f64(y, down, sum[0], 0, 0, 0);
+                        sum[e % 4] = __builtin_amdgcn_mfma_f64_4x4x4f64(x, q[0], sum[e % 4], 0, 0, 0);
+                        more[e % 4] = __builtin_amdgcn_mfma_f64_4x4x4f64(y, q[1], more[e % 4], 0, 0, 0);
                     } else {
-                        sum = __builtin_amdgcn_mfma_f64_16x16x4f64(x, up, sum, 0, 0, 0);
-                        sum = __builtin_amdgcn_mfma_f64_16x16x4f64(y, down, sum, 0, 0, 0);
+                        sum = __builtin_amdgcn_mfma_f64_16x16x4f64(x, q[0], sum, 0, 0, 0);
+                        more = __builtin_amdgcn_mfma_f64_16x16x4f64(y, q[1], more, 0, 0, 0);
                     }
                 }
+            sum += more;
+            if (COLS == 4) sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            // over the columns of a row, into its first: windows of twice the width, then one that ends where the row does
+            const uint64_t valid = __ballot(now.is);
+#pragma unroll
+            for (int r = 0; r < (COLS == 4 ? 1 : 4); ++r) {
+                double v = there ? fmax(sum[r], -INFINITY) : -INFINITY;       // (a sum that is no number: -infinity)
+                int w = 1;
+                for (; 2 * w <= window; w *= 2) v = fmax(v, __shfl(v, lane + w));
+                if (w < window) v = fmax(v, __shfl(v, lane + window - w));
+                // lane: 16x16x4 holds block 4 r + g, 4x4x4 block 4 (lane / 4 % 4) + g of query head lane % COLS
+                const int in = COLS == 4 ? lane / 4 % 4 * 4 + g : 4 * r + g, block = b0 + in;
+                if (col == row * window && row < rows && block < end_block) {
+                    uint64_t *to = a.scores + ((int64_t)(tile0 + row - a.row0) * a.kv_heads + head) * a.width + block;
+                    const uint64_t key = valid >> in & 1 ? key_of(v) : 0;
+                    *to = c && *to > key ? *to : key;
+                }
             }
-#pragma unroll
-            for (int r = 0; r < (COLS == 4 ? 1 : 4); ++r) best[r] = there ? fmax(best[r], sum[r]) : best[r];
-        }
-        // over the columns of a row, into its first: windows of twice the width, then one that ends where the row does
-        const int width = many == 1 ? window : COLS;
-        const uint64_t valid = __ballot(is);
-#pragma unroll
-        for (int r = 0; r < (COLS == 4 ? 1 : 4); ++r) {
-            double v = best[r];
-            int w = 1;
-            for (; 2 * w <= width; w *= 2) v = fmax(v, __shfl(v, lane + w));
-            if (w < width) v = fmax(v, __shfl(v, lane + width - w));
-            // lane: 16x16x4 holds block 4 r + g, 4x4x4 block 4 (lane / 4 % 4) + g of query head lane % COLS
-            const int in = COLS == 4 ? lane / 4 % 4 * 4 + g : 4 * r + g, block = b0 + in;
-            const int row = many == 1 ? col / a.group : 0;
-            if (col == row * width && row < rows && block < end_block)
-                a.scores[((int64_t)(tile0 + row - a.row0) * a.kv_heads + head) * a.width + block] = valid >> in & 1 ? key_of(v) : 0;
+        };
+        // two rounds at a time, so that bounds stay in the registers that they were loaded into
+        for (int b0 = begin; b0 < end_block; b0 += 128) {
+            round(b0, first, second);
+            if (b0 + 64 < end_block) round(b0 + 64, second, first);
         }
     }
 }
 
-// The `keep` largest keys of a row and head, the lowest blocks where keys are equal, in ascending order.  The smallest key kept is found bit by bit: each bit is one
-// count over the keys, which stay in registers.
+// Bits that any lane of a wavefront has.
+__device__ static inline uint32_t wave_or(uint32_t v) {
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);       // lanes xor 1
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);       // xor 2
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false);      // mirrored halves of a row
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false);      // mirrored row
+    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
+    return (row(0) | row(16)) | (row(32) | row(48));
+}
+
+// The `keep` largest keys of a row and head, the lowest blocks where keys are equal, in ascending order.  The smallest key kept is found bit by bit, from the
+// first that is not the same in all: each bit is one count over the keys, which stay in registers.
 template <int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS) void kv_pick(SelectArgs a) {
     constexpr int kWaves = THREADS / 64;
     __shared__ int counts[2][EACH][kWaves];
     __shared__ int total[2][kWaves];
+    __shared__ uint32_t bits[4][kWaves];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int row = a.row0 + (int)(blockIdx.x / a.kv_heads), head = blockIdx.x % a.kv_heads;
+    // (the scores of all of the table's columns do not wait for how many the row sees)
+    const uint64_t *scores = a.scores + ((int64_t)(row - a.row0) * a.kv_heads + head) * a.width;
+    uint64_t key[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) key[j] = scores[min(j * THREADS + t, a.width - 1)];
+    const int position = a.positions[row];
     Found f{};
     if (a.requests) f = last_place(a.requests, row, a.lengths, [&](int i) { return a.starts[i]; }, [](int, int start) { return (int64_t)start; });
     const int length = f.start <= row && row < f.end ? min(max(f.length, 0), a.width << a.block_log) : 0;
-    const int last = min(a.positions[row], length - 1), visible = last < 0 ? 0 : (last >> a.block_log) + 1;
-    const uint64_t *scores = a.scores + ((int64_t)(row - a.row0) * a.kv_heads + head) * a.width;
+    const int last = min(position, length - 1), visible = last < 0 ? 0 : (last >> a.block_log) + 1;
     int32_t *out = a.selected + ((int64_t)row * a.kv_heads + head) * a.keep;
-    uint64_t key[EACH];
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
         const int b = j * THREADS + t;
-        key[j] = b < visible ? scores[b] : 0;
-    }
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-        const int b = j * THREADS + t;
+        if (b >= visible) key[j] = 0;
         if (key[j] && (b < a.first || b >= visible - a.last)) key[j] = ~(uint64_t)0;
     }
     int turn = 0;
@@ -266,8 +316,29 @@ __global__ __launch_bounds__(THREADS) void kv_pick(SelectArgs a) {
     uint64_t least = 1;
     int kept = count(1);
     if (kept > a.keep) {
-        least = 0;
-        for (int bit = 63; bit >= 0; --bit) {
+        // (those that are always kept are all ones)
+        uint64_t set = 0, clear = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+            if (key[j] && ~key[j]) {
+                set |= key[j];
+                clear |= ~key[j];
+            }
+        uint32_t any[4] = {wave_or((uint32_t)set), wave_or((uint32_t)(set >> 32)), wave_or((uint32_t)clear), wave_or((uint32_t)(clear >> 32))};
+        if constexpr (kWaves > 1) {
+            if (lane < 4) bits[lane][wave] = lane == 0 ? any[0] : lane == 1 ? any[1] : lane == 2 ? any[2] : any[3];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) any[i] |= bits[i][w];
+        }
+        set = any[0] | (uint64_t)any[1] << 32;
+        const uint64_t differ = set & (any[2] | (uint64_t)any[3] << 32);
+        const int top = differ ? 63 - __builtin_clzll(differ) : -1;
+        least = top == 63 ? 0 : set & ~(((uint64_t)2 << max(top, 0)) - 1);
+        if (top < 0) least = set;                         // all the same
+        for (int bit = top; bit >= 0; --bit) {
             const uint64_t next = least | (uint64_t)1 << bit;
             const int n = count(next);
             if (n < a.keep) continue;
@@ -334,8 +405,10 @@ template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs 
     for (int row0 = 0; row0 < all; row0 += step) {
         a.row0 = row0;
         a.rows = all - row0 < step ? all - row0 : step;
-        const int64_t tiles = (int64_t)a.rows / a.tile_rows + a.requests;
-        int64_t blocks = 128;
+        const int64_t tiles = a.tile_rows == 1 ? a.rows : (int64_t)a.rows / a.tile_rows + a.requests;
+        // four rounds of a wavefront each, fewer where that leaves fewer than 1024 workgroups
+        int64_t blocks = 256;
+        while (blocks > 64 && tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) < 1024) blocks /= 2;
         while (tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) >= 1 << 24) blocks *= 2;
         a.chunk_blocks = (int)blocks;
         a.chunks = (int)((a.width + blocks - 1) / blocks);
