@@ -154,14 +154,55 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
     const int tiles = gridDim.x / (a.kv_heads * a.chunks), head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % tiles, chunk = rest / tiles;
     auto start_of = [&](int i) { return min(max(a.starts[i], a.row0), a.row0 + a.rows); };
     // a row at a time is found by itself; tiles of several begin at floor((starts[i] - row0) / tile_rows) + i
-    const bool single = a.tile_rows == 1;
+    const bool single = a.tile_rows == 1, wide = a.group > COLS;      // wide: a row's heads in several products
+    // (eight values a thread, neighbours to one place after the other)
+    constexpr int kParts = (COLS * 4 * kSteps + 255) / 256;
+    ElemVec<DT, 8> parts[kParts];
+    auto part_of = [&](int k, int &at, int &part, int &s) {
+        const int i = k * 256 + threadIdx.x;
+        at = i % COLS;
+        part = i / COLS % 4;
+        s = i / (COLS * 4);
+        return i < COLS * 4 * kSteps;
+    };
+    auto load_queries = [&](int c, int tile0, int rows) {
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            int at, part, s;
+            const bool is = part_of(k, at, part, s);
+            const int row = wide || single ? 0 : at / a.group, h = wide ? c * COLS + at : at - row * a.group;
+            parts[k] = ElemVec<DT, 8>{};
+            if (is && row < rows && h < a.group)
+                parts[k] = *reinterpret_cast<const ElemVec<DT, 8> *>(static_cast<const T *>(a.q) + ((int64_t)(tile0 + row) * a.q_heads + head * a.group + h) * DIM + s * 32 + part * 8);
+        }
+    };
+    auto fill_queries = [&] {
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            int at, part, s;
+            if (!part_of(k, at, part, s)) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = a.flip ? -(float)parts[k][e] : (float)parts[k][e];
+                queries[8 * s + e][part][at] = f64x2_t{(double)fmaxf(v, 0.f), (double)fminf(v, 0.f)};
+            }
+        }
+    };
+    int last = -1;                                                   // the last token that a row sees
+    if (single) {
+        load_queries(0, a.row0 + u, 1);
+        last = a.positions[a.row0 + u];
+    }
     const Found f = last_place(a.requests, single ? a.row0 + u : u, a.lengths, start_of,
                                [&](int i, int start) { return single ? (int64_t)start : (int64_t)((start - a.row0) / a.tile_rows) + i; });
     const int local = single ? a.row0 + u - f.start : u - ((f.start - a.row0) / a.tile_rows + f.request);
     const int tile0 = f.start + local * a.tile_rows, rows = min(f.end - tile0, a.tile_rows);
     if (local < 0 || rows <= 0) return;
     const int length = min(max(f.length, 0), a.width << a.block_log);
-    int last = lane < rows ? min(a.positions[tile0 + lane], length - 1) : -1;            // the last token that a row sees (16 rows at most)
+    if (!single) {
+        load_queries(0, tile0, rows);
+        last = lane < rows ? a.positions[tile0 + lane] : -1;          // (16 rows at most)
+    }
     // the first bounds do not wait for the positions: up to these, blocks of the request are read
     const int first_block = chunk * a.chunk_blocks, held_end = min(first_block + a.chunk_blocks, (length + (1 << a.block_log) - 1) >> a.block_log);
     if (first_block >= held_end) return;
@@ -179,15 +220,15 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
         }
     };
     const int begin = first_block + wave * 16, window = min(a.group, COLS);      // columns of a row
-    const bool wide = a.group > COLS;                     // a row's heads in several products
     Bounds first, second;
     int id_next = 0;
     if (begin < held_end) {
         load(begin, id_of(begin), first);
         id_next = id_of(min(begin + 64, held_end - 1));
     }
-    for (int s = 1; s < 16; s *= 2) last = max(last, __shfl_xor(last, s));
-    last = __builtin_amdgcn_readfirstlane(last);
+    if (!single)
+        for (int s = 1; s < 16; s *= 2) last = max(last, __shfl_xor(last, s));
+    last = min(__builtin_amdgcn_readfirstlane(last), length - 1);
     const int end_block = min(held_end, last < 0 ? 0 : (last >> a.block_log) + 1);
     if (first_block >= end_block) return;
     for (int c = 0; c * COLS < (wide ? a.group : 1); ++c) {
@@ -198,18 +239,8 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
                 id_next = id_of(min(begin + 64, held_end - 1));
             }
         }
-        // (eight values a thread, neighbours to one place after the other)
-        for (int i = threadIdx.x; i < COLS * 4 * kSteps; i += 256) {
-            const int at = i % COLS, part = i / COLS % 4, s = i / (COLS * 4), pair = c * COLS + at, row = wide ? 0 : at / a.group, h = wide ? pair : at % a.group;
-            ElemVec<DT, 8> q = {};
-            if (row < rows && h < a.group)
-                q = *reinterpret_cast<const ElemVec<DT, 8> *>(static_cast<const T *>(a.q) + ((int64_t)(tile0 + row) * a.q_heads + head * a.group + h) * DIM + s * 32 + part * 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = a.flip ? -(float)q[e] : (float)q[e];
-                queries[8 * s + e][part][at] = f64x2_t{(double)fmaxf(v, 0.f), (double)fminf(v, 0.f)};
-            }
-        }
+        if (c) load_queries(c, tile0, rows);
+        fill_queries();
         __syncthreads();
         const int pair = c * COLS + col, row = wide ? 0 : col / a.group;
         const bool there = wide ? pair < a.group : row < rows;
