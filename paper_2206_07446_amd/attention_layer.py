@@ -1,8 +1,10 @@
 """One attention layer of a language model as a serving program runs it, from request lengths to the layer's output
 rows: the cold start (weights to 8 bits), a step that takes the requests' prompts in, and steps of one token a request
-replayed from a HIP graph.  The layer keeps every buffer, so that a step is seven calls and no allocation.
+replayed from a HIP graph.  The layer keeps every buffer, so that a step is seven calls and no allocation.  Its attention is over the whole cache, over
+the blocks that each row selects (`keep`), or over prefixes that groups of requests share (`share`); `step_stream` runs it from the residual
+stream to the residual stream and the norm for the next layer.
 
-`python -m paper_2206_07446_amd.attention_layer --requests 64 --prompt 512 --steps 64` prints the time of each part.
+`python -m paper_2206_07446_amd.attention_layer --requests 64 --prompt 512 --steps 64` prints the time of each part; with `--keep 8` or `--shared 4096` too.
 """
 from __future__ import annotations
 
@@ -16,10 +18,14 @@ DTYPES = {nnv.F16: torch.float16, nnv.BF16: torch.bfloat16}
 
 
 class AttentionLayer:
-    """Weights, cache, block table and buffers for up to `rows` rows a step and `requests` requests of `tokens` tokens (whole blocks of them)."""
+    """Weights, cache, block table and buffers for up to `rows` rows a step and `requests` requests of `tokens` tokens (whole blocks of them).
+    keep: a row sees so many blocks, the first `first`, the last `last` and those of the largest scores; 0: all.  groups: the most groups of requests that may share a prefix."""
 
     def __init__(self, hidden, q_heads, kv_heads, head_dim, requests, rows, tokens, block_tokens=64, dtype=nnv.BF16, theta=10000.0, window=0, sinks=0,
-                 device="cuda:0"):
+                 device="cuda:0", keep=0, first=1, last=2, groups=0):
+        if keep and (window or groups or not 0 <= first + last <= keep or min(first, last) < 0):
+            raise ValueError("blocks are selected without a window and shared prefixes, the first and last ones among those kept")
+        self.keep, self.first, self.last, self.groups, self.n_groups = keep, first, last, groups, 0
         self.device, self.dtype, self.requests, self.rows, self.hidden = torch.device(device), DTYPES[dtype], requests, rows, hidden
         width = -(-tokens // block_tokens)
         self.desc = nnv.AttentionDesc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, block_tokens=block_tokens, blocks=requests * width,
@@ -35,7 +41,17 @@ class AttentionLayer:
         # what a call over m rows needs of its scratch goes up and down with m, where the number of parts that it splits into changes: the most of every size
         need = max(max(nnv.nnv_kv_attention_workspace_bytes(self.desc, requests, m), *(nnv.nnv_linear_workspace_bytes(d, m) for d in (self.qkv_desc, self.out_desc)))
                    for m in range(1, rows + 1))
+        if keep:
+            self.bounds = torch.zeros(nnv.nnv_kv_bounds_bytes(self.desc) // 2, dtype=torch.bfloat16, device=self.device)
+            self.selected = new(rows, kv_heads, keep, dtype=torch.int32)
+            need = max(need, *(max(nnv.nnv_kv_select_workspace_bytes(self.desc, requests, m), nnv.nnv_kv_attention_blocks_workspace_bytes(self.desc, requests, m, keep))
+                               for m in range(1, rows + 1)))
+        if groups:
+            need = max(need, *(nnv.nnv_kv_attention_shared_workspace_bytes(self.desc, requests, m, g) for m in range(1, rows + 1) for g in range(1, groups + 1)))
+            self.group_ends, self.shared = (torch.zeros(groups + n, dtype=torch.int32, device=self.device) for n in (1, 0))
         self.workspace = bytes_(need)
+        self.norm_in, self.norm_next, self.norm_out = (torch.ones(hidden, device=self.device) for _ in range(3))
+        self.out = new(rows, hidden)
         self.q_weight, self.k_weight = (torch.ones(head_dim, device=self.device) for _ in range(2))
         half = head_dim // 2
         angle = torch.arange(width * block_tokens, dtype=torch.float64)[:, None] * theta ** (-torch.arange(half, dtype=torch.float64) / half)
@@ -81,8 +97,36 @@ class AttentionLayer:
         nnv.nnv_qk_norm_rope(self.desc, rows, q, stride, k, stride, v, stride, self.q_weight, self.k_weight, self.rope, self.positions, self.slots, self.q,
                              None, self.cache)
 
+    def share(self, ends, tokens):
+        """Requests ends[g] to ends[g + 1] - 1 begin with the same tokens[g] tokens (whole blocks), which the first of them holds; the others hold nothing yet, and
+        from here on begin behind them.  No groups: nothing is shared any more by requests that begin later."""
+        ends, tokens, block = list(ends), list(tokens), self.desc.block_tokens
+        held = self.held.tolist()
+        if len(tokens) > self.groups or len(ends) != len(tokens) + 1 or sorted(ends) != ends or ends[0] < 0 or ends[-1] > self.requests:
+            raise ValueError(f"expected up to {self.groups} groups of the {self.requests} requests, in their order")
+        for first, end, n in zip(ends, ends[1:], tokens):
+            if n < 0 or n % block or (first < end and held[first] < n) or any(held[i] for i in range(first + 1, end)):
+                raise ValueError(f"{n} tokens: expected whole blocks of {block} that request {first} holds, and nothing held by the others of its group")
+        for first, end, n in zip(ends, ends[1:], tokens):
+            self.held[first + 1:end] = n
+        if tokens:
+            self.group_ends[:len(ends)] = torch.tensor(ends, dtype=torch.int32)
+            self.shared[:len(tokens)] = torch.tensor(tokens, dtype=torch.int32)
+        self.n_groups = len(tokens)
+
     def attend(self, rows):
         self._check(rows)
+        if self.keep:
+            nnv.nnv_kv_bounds(self.desc, self.requests, rows, self.table, self.starts, self.lengths, self.cache, self.bounds)
+            nnv.nnv_kv_select(self.desc, self.requests, rows, self.keep, self.first, self.last, self.q, self.table, self.starts, self.lengths, self.positions,
+                              self.bounds, self.selected, self.workspace)
+            nnv.nnv_kv_attention_blocks(self.desc, self.requests, rows, self.keep, self.q, self.table, self.starts, self.lengths, self.positions, self.selected,
+                                        self.cache, self.attended, self.workspace)
+            return
+        if self.n_groups:
+            nnv.nnv_kv_attention_shared(self.desc, self.requests, rows, self.n_groups, self.q, self.table, self.starts, self.lengths, self.positions,
+                                        self.group_ends, self.shared, self.cache, self.attended, self.workspace)
+            return
         nnv.nnv_kv_attention(self.desc, self.requests, rows, self.q, self.table, self.starts, self.lengths, self.positions, self.cache, self.attended,
                              self.workspace)
 
@@ -102,6 +146,27 @@ class AttentionLayer:
         self.held.copy_(self.lengths)
         self.count.copy_(self.left)
 
+    def step_stream(self, x, h, rows, begin=False, post=False, gate=None, index=None, scale=1.0):
+        """A step on the residual stream x (rows of float32 or 16 bits, updated in place).  h: rows of the layer's type, in it this layer's input as the layer
+        before left it (begin: the norm of x by norm_in is taken first), after it the norm by norm_next of the new stream.  What is added is the layer's output,
+        behind a norm by norm_out where post is set, times scale and its row of gate, or row index[i] of it."""
+        self._check(rows, h)
+        types = {torch.float32: nnv.F32, torch.float16: nnv.F16, torch.bfloat16: nnv.BF16}
+        if not (isinstance(x, torch.Tensor) and x.dtype in types and x.device == self.qkv.device and x.dim() == 2 and x.shape[0] >= rows and x.shape[1] == self.hidden
+                and x.stride(1) == 1 and (rows <= 1 or x.stride(0) >= self.hidden) and x.data_ptr() % 16 == 0):
+            raise ValueError(f"expected a stream of {rows} rows or more of {self.hidden} values on {self.qkv.device}, each without gaps, the first 16-byte aligned")
+        gates, stride = (0, 0) if gate is None else (gate.shape[0], gate.stride(0))
+        if gate is not None and not (gate.dtype == self.dtype and gate.device == self.qkv.device and gate.dim() == 2 and gate.shape[1] == self.hidden and gate.stride(1) == 1):
+            raise ValueError(f"expected gates of {self.hidden} {self.dtype} on {self.qkv.device}")
+        if index is not None and not (index.dtype == torch.int32 and index.device == self.qkv.device and index.is_contiguous() and index.numel() >= rows):
+            raise ValueError(f"expected {rows} int32 or more on {self.qkv.device}")
+        desc = nnv.ResidualDesc(n=self.hidden, x_dtype=types[x.dtype], y_dtype=self.desc.dtype, h_dtype=self.desc.dtype, scale=scale, eps=self.desc.eps)
+        if begin:
+            nnv.nnv_residual_norm(desc, rows, x, x.stride(0), None, 0, None, 0, None, 0, None, self.norm_in, None, 0, h, h.stride(0))
+        self.step(h, self.out, rows)
+        nnv.nnv_residual_norm(desc, rows, x, x.stride(0), self.out, self.out.stride(0), self.norm_out if post else None, gates, gate, stride, index, self.norm_next,
+                              x, x.stride(0), h, h.stride(0))
+
 
 def _time(f, reps):
     a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
@@ -117,10 +182,13 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     for name, value in (("hidden", 4096), ("q-heads", 32), ("kv-heads", 8), ("head-dim", 128), ("requests", 64), ("prompt", 512), ("steps", 64)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--keep", type=int, default=0, help="blocks of 64 tokens that a row sees (0: all)")
+    ap.add_argument("--shared", type=int, default=0, help="tokens that all requests begin with, in whole blocks of 64")
     a = ap.parse_args(argv)
     torch.manual_seed(220607446)
-    rows = a.requests * a.prompt
-    layer = AttentionLayer(a.hidden, a.q_heads, a.kv_heads, a.head_dim, a.requests, rows, a.prompt + a.steps + 8)
+    rows = max(a.requests * a.prompt, a.shared)
+    layer = AttentionLayer(a.hidden, a.q_heads, a.kv_heads, a.head_dim, a.requests, rows, a.shared + a.prompt + a.steps + 8, keep=a.keep, last=min(2, a.keep - 1) if a.keep else 2,
+                           groups=1 if a.shared else 0)
     dev = layer.device
     w_qkv = torch.randn(layer.qkv_desc.n, a.hidden, device=dev) * a.hidden ** -0.5
     w_out = torch.randn(a.hidden, layer.q_size, device=dev) * layer.q_size ** -0.5
@@ -129,15 +197,21 @@ def main(argv=None):
     layer.transform_weights(w_qkv, w_out)                    # the library and the GPU are awake after this
     torch.cuda.synchronize()
     print(f"weights to 8 bits        {_time(lambda: layer.transform_weights(w_qkv, w_out), 3):10.1f} us")
+    if a.shared:
+        layer.fresh[0] = a.shared
+        print(f"prefix,  {a.shared:7d} rows    {_time(lambda: layer.step(x, y, a.shared), 1):10.1f} us")
+        layer.share([0, a.requests], [a.shared])
     layer.fresh.fill_(a.prompt)
+    rows = a.requests * a.prompt
     print(f"prompts, {rows:7d} rows    {_time(lambda: layer.step(x, y, rows), 1):10.1f} us")
     layer.fresh.fill_(1)
     n = a.requests
     layer.step(x, y, n)
     torch.cuda.synchronize()
+    stream, h = x[:n].float(), x[:n].clone()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        layer.step(x, y, n)
+        layer.step_stream(stream, h, n)
     print(f"a token, {n:7d} rows    {_time(graph.replay, a.steps):10.1f} us a replayed step")
     for name, part in (("plan", lambda: layer.plan(n)), ("project", lambda: layer.project(x, n)), ("append", lambda: layer.append(n)),
                        ("attend", lambda: layer.attend(n)), ("finish", lambda: layer.finish(y, n))):
