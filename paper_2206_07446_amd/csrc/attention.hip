@@ -206,7 +206,16 @@ template <int R, int S> __device__ static inline Part find_part(const AttendArgs
     }
     // (each tile's last part counts as one more; rounded up by more than the sum is off: no more parts than there are workgroups)
     const float units = fmaxf(a.prefix_units - whole, 0.5f * a.prefix_units);
-    const int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / units), 1e9f));
+    int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / units), 1e9f));
+    if (a.n_groups <= 16) {
+        // of 64 lengths from the shortest that could do, a lane each, the first that gives no more parts than that
+        const int shortest = max(a.prefix_least, (int)fminf(ceilf(total / a.prefix_units), 1e9f)), tried = shortest + lane * ((shortest + 63) / 64);
+        float parts = 0;
+        for (int g = 0; g < a.n_groups; ++g)
+            parts += (float)__builtin_amdgcn_readlane(tiles, g) * (float)min((__builtin_amdgcn_readlane(steps, g) + tried - 1) / tried, a.prefix_splits);
+        const uint64_t fits = __ballot(parts <= a.prefix_units);
+        if (fits) each = __builtin_amdgcn_readlane(tried, __builtin_ctzll(fits));
+    }
     const int splits = min((steps + each - 1) / each, a.prefix_splits), parts = tiles * splits;
     int before = 0, sum = parts;
     for (int s = 1; s < 64; s *= 2) {
@@ -386,7 +395,8 @@ constexpr int kFewest = 512;       // tokens of a split at least, where the host
 template <int DIM> using FewJoin = float[kAttendWaves][kTileRows][DIM / 2 + 4];
 using FewSums = float[kAttendWaves][kTileRows];
 
-template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(const AttendArgs &a, int group, FewJoin<DIM> &join, FewSums &join_base, FewSums &join_sum) {
+// DEPTH: steps of a wavefront that are on their way while it computes one.
+template <int DT, int DIM, int SEEN, int DEPTH> __device__ static inline void attend_few(const AttendArgs &a, int group, FewJoin<DIM> &join, FewSums &join_base, FewSums &join_sum) {
     typedef typename Elem<DT>::type T;
     constexpr int kQ = DIM / 32, kJ = DIM / 16;          // instructions of a score, of an output
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane % 16, g = lane / 16;
@@ -454,8 +464,8 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(co
     const TableRow table = table_row(a, SEEN == kPrefix ? leader_of(a, t.request) : t.request);
     // the last step of this wavefront is loaded again where there is no next one: a load that some rounds leave out would
     // make every round wait for all that are on their way
-    Held<DIM> held_a, held_b;
-    StepBlocks blocks = {{-1, -1}, {}}, next_blocks = {{-1, -1}, {}};
+    Held<DIM> held_steps[DEPTH + 1];
+    StepBlocks blocks = {{-1, -1}, {}}, next_blocks[DEPTH];        // of the step that is computed, of those after it
     const int first = begin + wave, last = first + (end - 1 - first) / kAttendWaves * kAttendWaves;
     // Of a list, the blocks of 32 rounds at a time are looked up, two lanes a round: list and table are a chain that no round should wait for.
     int entry_id = -1, entry_token = 0, entries_from = -1;
@@ -482,8 +492,11 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(co
     };
     if (first < end) {
         blocks = step_blocks(first);
-        next_blocks = step_blocks(min(first + kAttendWaves, last));
-        load_step<DIM>(a, head, number_of<SEEN>(steps.at(first)), blocks, held_a);
+#pragma unroll
+        for (int k = 0; k < DEPTH; ++k) next_blocks[k] = step_blocks(min(first + (k + 1) * kAttendWaves, last));
+        load_step<DIM>(a, head, number_of<SEEN>(steps.at(first)), blocks, held_steps[0]);
+#pragma unroll
+        for (int k = 1; k < DEPTH; ++k) load_step<DIM>(a, head, number_of<SEEN>(steps.at(min(first + k * kAttendWaves, last))), next_blocks[k - 1], held_steps[k]);
     }
     const int highest = uniform(row_max(own)), lowest = -uniform(row_max(there ? -max(own, -1) : -0x7fffffff));
     const int tokens = SEEN == kBoth ? max(t.length, from) : t.length;
@@ -498,8 +511,8 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(co
     __builtin_amdgcn_s_waitcnt(0xf70);                    // vmcnt 0: the queries are here before the rounds begin
     auto round = [&](int i, Held<DIM> &held, Held<DIM> &next) {
         const int step = steps.at(i);
-        load_step<DIM>(a, head, number_of<SEEN>(steps.at(min(i + kAttendWaves, last))), next_blocks, next);
-        const StepBlocks later = step_blocks(min(i + 2 * kAttendWaves, last));
+        load_step<DIM>(a, head, number_of<SEEN>(steps.at(min(i + DEPTH * kAttendWaves, last))), next_blocks[DEPTH - 1], next);
+        const StepBlocks later = step_blocks(min(i + (DEPTH + 1) * kAttendWaves, last));
         f32x4_t s[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -575,16 +588,23 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_few(co
             o[2 * jj] = Mfma<DT>::dot(even, weights, o[2 * jj]);
             o[2 * jj + 1] = Mfma<DT>::dot(odd, weights, o[2 * jj + 1]);
         }
-        blocks = next_blocks;
-        next_blocks = later;
+        blocks = next_blocks[0];
+#pragma unroll
+        for (int k = 1; k < DEPTH; ++k) next_blocks[k - 1] = next_blocks[k];
+        next_blocks[DEPTH - 1] = later;
     };
-    // two rounds at a time, so that codes stay in the registers that they were loaded into
+    // as many rounds at a time as there are steps in registers, so that codes stay in those that they were loaded into
     for (int i = first; i < end;) {
-        round(i, held_a, held_b);
+        round(i, held_steps[0], held_steps[DEPTH]);
         i += kAttendWaves;
         if (i >= end) break;
-        round(i, held_b, held_a);
+        round(i, held_steps[1], held_steps[0]);
         i += kAttendWaves;
+        if constexpr (DEPTH == 2) {
+            if (i >= end) break;
+            round(i, held_steps[2], held_steps[1]);
+            i += kAttendWaves;
+        }
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -630,7 +650,7 @@ template <int DT, int DIM, int SEEN>
 __global__ __launch_bounds__(64 * kAttendWaves, DIM == 256 ? 2 : 4) void kv_attend(AttendArgs a) {
     __shared__ FewJoin<DIM> join;
     __shared__ FewSums join_base, join_sum;
-    attend_few<DT, DIM, SEEN>(a, blockIdx.x, join, join_base, join_sum);
+    attend_few<DT, DIM, SEEN, 1>(a, blockIdx.x, join, join_base, join_sum);
 }
 
 // Requests of many rows: a workgroup holds 128 pairs, 32 to a wavefront, and goes over the tokens 64 at a time.  Each wavefront turns the codes of 16
@@ -980,10 +1000,10 @@ __global__ __launch_bounds__(256, MANY ? (DIM == 256 ? 1 : DIM == 128 ? 2 : 3) :
     if constexpr (MANY) {
         if (group < a.prefix_groups) attend_many_rows<DT, DIM, kPrefix>(a, group, lds.many.keys, lds.many.values);
         else if (group < a.prefix_groups + a.own_many) attend_many_rows<DT, DIM, kOwn>(a, group - a.prefix_groups, lds.many.keys, lds.many.values);
-        else attend_few<DT, DIM, kOwn>(a, group - a.prefix_groups - a.own_many, lds.few.join, lds.few.base, lds.few.sum);
+        else attend_few<DT, DIM, kOwn, 2>(a, group - a.prefix_groups - a.own_many, lds.few.join, lds.few.base, lds.few.sum);
     } else {
-        if (group < a.prefix_groups) attend_few<DT, DIM, kPrefix>(a, group, lds.few.join, lds.few.base, lds.few.sum);
-        else attend_few<DT, DIM, kOwn>(a, group - a.prefix_groups, lds.few.join, lds.few.base, lds.few.sum);
+        if (group < a.prefix_groups) attend_few<DT, DIM, kPrefix, 1>(a, group, lds.few.join, lds.few.base, lds.few.sum);
+        else attend_few<DT, DIM, kOwn, 1>(a, group - a.prefix_groups, lds.few.join, lds.few.base, lds.few.sum);
     }
 }
 
@@ -1235,12 +1255,13 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
     };
     const int64_t tile = s.many ? kManyRows : kTileRows, prefix_tiles = pairs / tile + groups + 1;
     if (groups) {
-        const int64_t target = 512;
+        const int64_t target = 384;
         s.units = (int)((target + d.kv_heads - 1) / d.kv_heads);
         s.least = s.many ? 8 : 4;
         if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
         else s.prefix = within(s.units, capacity / 128 + 1);
-        s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : s.units + prefix_tiles) * d.kv_heads;
+        // (parts are no more than units where tiles are no more than half of those: see find_part)
+        s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : prefix_tiles <= s.units / 2 ? s.units : s.units + prefix_tiles) * d.kv_heads;
     }
     const int64_t own_tile = own_many ? kManyRows : kTileRows, full = pairs / own_tile, least = requests < rows ? requests : rows;
     const int64_t own_tiles = (full > least ? full : least > 0 ? least : 1) * d.kv_heads;
