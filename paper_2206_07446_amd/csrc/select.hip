@@ -131,6 +131,8 @@ hipError_t launch_kv_bounds(const BoundsArgs &a, int dim, hipStream_t st) {
 // ---- selection ----------------------------------------------------------------------------------
 
 typedef double f64x2_t __attribute__((ext_vector_type(2)));
+constexpr int kMostKeys = 4096;                          // of a tile's rows, where one workgroup scores and picks
+
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
 // Numbers in the order of 64-bit keys; a NaN counts as -infinity.  Key 0 is no block's.
@@ -140,26 +142,102 @@ __device__ static inline uint64_t key_of(double v) {
     return bits >> 63 ? ~bits : bits | (uint64_t)1 << 63;
 }
 
+// Bits that any lane of a wavefront has.
+__device__ static inline uint32_t wave_or(uint32_t v) {
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);       // lanes xor 1
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);       // xor 2
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false);      // mirrored halves of a row
+    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false);      // mirrored row
+    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
+    return (row(0) | row(16)) | (row(32) | row(48));
+}
+
+// The `keep` largest of `visible` keys, the lowest blocks where keys are equal, in ascending order, by a wavefront whose lanes hold EACH of them.  The smallest key
+// kept is found bit by bit, from the first that is not the same in all: each bit is one count over the keys.
+template <int EACH> __device__ static inline void pick_by_wave(const uint64_t *keys, int visible, int first, int last, int keep, int32_t *out) {
+    const int lane = threadIdx.x & 63;
+    uint64_t key[EACH], set = 0, clear = 0;
+    int kept = 0;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int b = j * 64 + lane;
+        key[j] = b < visible ? keys[b] : 0;
+        if (key[j] && (b < first || b >= visible - last)) key[j] = ~(uint64_t)0;
+        if (key[j] && ~key[j]) {                          // (those that are always kept are all ones)
+            set |= key[j];
+            clear |= ~key[j];
+        }
+        kept += __builtin_popcountll(__ballot(key[j] != 0));
+    }
+    auto count = [&](uint64_t least) {
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) n += __builtin_popcountll(__ballot(key[j] >= least));
+        return n;
+    };
+    uint64_t least = 1;
+    if (kept > keep) {
+        set = wave_or((uint32_t)set) | (uint64_t)wave_or((uint32_t)(set >> 32)) << 32;
+        const uint64_t differ = set & (wave_or((uint32_t)clear) | (uint64_t)wave_or((uint32_t)(clear >> 32)) << 32);
+        const int top = differ ? 63 - __builtin_clzll(differ) : -1;
+        least = top < 0 ? set : top == 63 ? 0 : set & ~(((uint64_t)2 << top) - 1);
+        for (int bit = top; bit >= 0; --bit) {
+            const uint64_t next = least | (uint64_t)1 << bit;
+            const int n = count(next);
+            if (n < keep) continue;
+            least = next;
+            kept = n;
+            if (n == keep) break;
+        }
+    }
+    // of the keys that are `least`, so many as fit are taken, the first ones
+    int equal = kept > keep ? keep - count(least + 1) : 0x7fffffff, place = 0;      // (a key of all ones cannot be one too many: first + last <= keep)
+    const uint64_t before = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const uint64_t same = __ballot(key[j] == least);
+        const bool take = key[j] > least || (key[j] == least && __builtin_popcountll(same & before) < equal);
+        const uint64_t taken = __ballot(take);
+        if (take) out[place + __builtin_popcountll(taken & before)] = j * 64 + lane;
+        place += __builtin_popcountll(taken);
+        equal -= __builtin_popcountll(same);
+    }
+    for (int i = place + lane; i < keep; i += 64) out[i] = -1;
+}
+
 // Scores of a tile of whole rows with a head's blocks: max(q hi, q lo) is max(q, 0) hi + min(q, 0) lo, so that a score is one product over 2 DIM, on the
 // matrix cores in float64: 16 blocks x 4 values x 4 query heads (4x4x4, four of them in an instruction) or x 16 (16x16x4).  Lane l holds of block, and of query
 // head, l % 16 (l % 4) the eight values from 32 s + 8 (l / 16): products sum over values in any order.  Queries lie in the LDS as they enter, the same for all
 // wavefronts; the bounds of a wavefront's next 16 blocks are on their way while it computes.
-template <int DT, int DIM, int COLS>
-__global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_scores(SelectArgs a) {
+//
+// EACH: where it is not 0, a workgroup of eight wavefronts takes all blocks of its tile (up to 64 EACH of a row), keeps their keys in the LDS and picks from them, a
+// wavefront a row; otherwise one of four takes a chunk of the blocks and keys go to memory, for kv_pick.
+template <int DT, int DIM, int COLS, int EACH>
+__global__ __launch_bounds__(EACH ? 512 : 256, DIM == 256 ? 2 : EACH ? 4 : DIM == 128 ? 3 : 4) void kv_scores(SelectArgs a) {
     typedef typename Elem<DT>::type T;
-    constexpr int kSteps = DIM / 32;
+    constexpr int kSteps = DIM / 32, kThreads = EACH ? 512 : 256, kRound = kThreads / 4;      // kRound: blocks that the wavefronts take at a time
+    constexpr bool kPick = EACH != 0;
+    __shared__ uint64_t keys[kPick ? kMostKeys : 1];
     __shared__ f64x2_t queries[DIM / 4][4][COLS];                    // max(q, 0) and min(q, 0) of value 32 s + 8 g + e at [8 s + e][g]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane / 16, col = lane % COLS;
     // (chunks last: workgroups go to the chip's eight parts in turn, and of two chunks the second, which fewer requests reach, would keep half of them idle)
-    const int tiles = gridDim.x / (a.kv_heads * a.chunks), head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % tiles, chunk = rest / tiles;
+    const int tiles = a.tiles, head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, u = rest % tiles, chunk = rest / tiles;
+    if (kPick && rest >= tiles) {                        // (rows of no request are in no tile)
+        const int begin = min(max(a.starts[0], 0), a.rows), end = min(max(a.starts[a.requests], 0), a.rows);
+        const int64_t each = (int64_t)a.kv_heads * a.keep;
+        for (int row = blockIdx.x - tiles * a.kv_heads; row < a.rows; row += a.kv_heads)
+            if (row < begin || row >= end)
+                for (int64_t i = threadIdx.x; i < each; i += kThreads) a.selected[row * each + i] = -1;
+        return;
+    }
     auto start_of = [&](int i) { return min(max(a.starts[i], a.row0), a.row0 + a.rows); };
     // a row at a time is found by itself; tiles of several begin at floor((starts[i] - row0) / tile_rows) + i
     const bool single = a.tile_rows == 1, wide = a.group > COLS;      // wide: a row's heads in several products
     // (eight values a thread, neighbours to one place after the other)
-    constexpr int kParts = (COLS * 4 * kSteps + 255) / 256;
+    constexpr int kParts = (COLS * 4 * kSteps + kThreads - 1) / kThreads;
     ElemVec<DT, 8> parts[kParts];
     auto part_of = [&](int k, int &at, int &part, int &s) {
-        const int i = k * 256 + threadIdx.x;
+        const int i = k * kThreads + threadIdx.x;
         at = i % COLS;
         part = i / COLS % 4;
         s = i / (COLS * 4);
@@ -197,7 +275,11 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
                                [&](int i, int start) { return single ? (int64_t)start : (int64_t)((start - a.row0) / a.tile_rows) + i; });
     const int local = single ? a.row0 + u - f.start : u - ((f.start - a.row0) / a.tile_rows + f.request);
     const int tile0 = f.start + local * a.tile_rows, rows = min(f.end - tile0, a.tile_rows);
-    if (local < 0 || rows <= 0) return;
+    if (local < 0 || rows <= 0) {
+        if (kPick && single)
+            for (int i = threadIdx.x; i < a.keep; i += kThreads) a.selected[((int64_t)(a.row0 + u) * a.kv_heads + head) * a.keep + i] = -1;
+        return;
+    }
     const int length = min(max(f.length, 0), a.width << a.block_log);
     if (!single) {
         load_queries(0, tile0, rows);
@@ -205,7 +287,7 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
     }
     // the first bounds do not wait for the positions: up to these, blocks of the request are read
     const int first_block = chunk * a.chunk_blocks, held_end = min(first_block + a.chunk_blocks, (length + (1 << a.block_log) - 1) >> a.block_log);
-    if (first_block >= held_end) return;
+    if (!kPick && first_block >= held_end) return;
     const int32_t *table = a.table + (int64_t)f.request * a.width;
 
     struct Bounds { i32x4_t hi[kSteps], lo[kSteps]; bool is; };
@@ -224,19 +306,20 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
     int id_next = 0;
     if (begin < held_end) {
         load(begin, id_of(begin), first);
-        id_next = id_of(min(begin + 64, held_end - 1));
+        id_next = id_of(min(begin + kRound, held_end - 1));
     }
+    const int seen = min(last, length - 1);               // of row `lane` (of the only one, in all lanes)
     if (!single)
         for (int s = 1; s < 16; s *= 2) last = max(last, __shfl_xor(last, s));
     last = min(__builtin_amdgcn_readfirstlane(last), length - 1);
     const int end_block = min(held_end, last < 0 ? 0 : (last >> a.block_log) + 1);
-    if (first_block >= end_block) return;
+    if (!kPick && first_block >= end_block) return;
     for (int c = 0; c * COLS < (wide ? a.group : 1); ++c) {
         if (c) {
             __syncthreads();
             if (begin < end_block) {
                 load(begin, id_of(begin), first);
-                id_next = id_of(min(begin + 64, held_end - 1));
+                id_next = id_of(min(begin + kRound, held_end - 1));
             }
         }
         if (c) load_queries(c, tile0, rows);
@@ -245,9 +328,9 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
         const int pair = c * COLS + col, row = wide ? 0 : col / a.group;
         const bool there = wide ? pair < a.group : row < rows;
         auto round = [&](int b0, const Bounds &now, Bounds &next) {
-            const int after = min(b0 + 64, held_end - 1);            // (behind the last block, that one again)
+            const int after = min(b0 + kRound, held_end - 1);        // (behind the last block, that one again)
             load(after, id_next, next);
-            id_next = id_of(min(after + 64, held_end - 1));
+            id_next = id_of(min(after + kRound, held_end - 1));
             asm volatile("" ::: "memory");             // queries are read again each round: kept, they would take the registers of another wavefront
             f64x4_t sum = {0, 0, 0, 0}, more = {0, 0, 0, 0};
 #pragma unroll
@@ -279,28 +362,26 @@ __global__ __launch_bounds__(256, DIM == 256 ? 2 : DIM == 128 ? 3 : 4) void kv_s
                 // lane: 16x16x4 holds block 4 r + g, 4x4x4 block 4 (lane / 4 % 4) + g of query head lane % COLS
                 const int in = COLS == 4 ? lane / 4 % 4 * 4 + g : 4 * r + g, block = b0 + in;
                 if (col == row * window && row < rows && block < end_block) {
-                    uint64_t *to = a.scores + ((int64_t)(tile0 + row - a.row0) * a.kv_heads + head) * a.width + block;
+                    uint64_t *to = kPick ? keys + row * a.width + block : a.scores + ((int64_t)(tile0 + row - a.row0) * a.kv_heads + head) * a.width + block;
                     const uint64_t key = valid >> in & 1 ? key_of(v) : 0;
                     *to = c && *to > key ? *to : key;
                 }
             }
         };
         // two rounds at a time, so that bounds stay in the registers that they were loaded into
-        for (int b0 = begin; b0 < end_block; b0 += 128) {
+        for (int b0 = begin; b0 < end_block; b0 += 2 * kRound) {
             round(b0, first, second);
-            if (b0 + 64 < end_block) round(b0 + 64, second, first);
+            if (b0 + kRound < end_block) round(b0 + kRound, second, first);
         }
     }
-}
-
-// Bits that any lane of a wavefront has.
-__device__ static inline uint32_t wave_or(uint32_t v) {
-    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);       // lanes xor 1
-    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);       // xor 2
-    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false);      // mirrored halves of a row
-    v |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false);      // mirrored row
-    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
-    return (row(0) | row(16)) | (row(32) | row(48));
+    if constexpr (kPick) {
+        __syncthreads();
+        for (int r = wave; r < rows; r += kThreads / 64) {
+            const int own = __builtin_amdgcn_readlane(seen, r);
+            pick_by_wave<EACH>(keys + r * a.width, own < 0 ? 0 : (own >> a.block_log) + 1, a.first, a.last, a.keep,
+                               a.selected + ((int64_t)(tile0 + r) * a.kv_heads + head) * a.keep);
+        }
+    }
 }
 
 // The `keep` largest keys of a row and head, the lowest blocks where keys are equal, in ascending order.  The smallest key kept is found bit by bit, from the
@@ -437,16 +518,29 @@ template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs 
         a.row0 = row0;
         a.rows = all - row0 < step ? all - row0 : step;
         const int64_t tiles = a.tile_rows == 1 ? a.rows : (int64_t)a.rows / a.tile_rows + a.requests;
-        // four rounds of a wavefront each, fewer where that leaves fewer than 1024 workgroups
-        int64_t blocks = 256;
-        while (blocks > 64 && tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) < 1024) blocks /= 2;
+        a.tiles = (int)tiles;
+        // One launch for single rows of up to 1024 blocks that keep the chip busy with a workgroup each (64 rows over up to 512 blocks 30.0 -> 26.4 us), and wherever there
+        // is little to do; not for prompts, whose scores wait for the matrix cores (1000 rows over up to 282 blocks: 49 us, in two launches 36).
+        const int64_t units = tiles * a.kv_heads;
+        if (a.requests && a.width <= 1024 && a.width * a.tile_rows <= kMostKeys && (narrow ? units >= 256 || a.width <= 256 : units < 512 && a.width <= 256) && all == a.rows) {
+            a.chunks = 1;
+            a.chunk_blocks = a.width;
+            const unsigned picks = (unsigned)((tiles + (a.tile_rows > 1)) * a.kv_heads);
+            if (a.width <= 512) narrow ? kv_scores<DT, DIM, 4, 8><<<picks, 512, 0, st>>>(a) : kv_scores<DT, DIM, 16, 8><<<picks, 512, 0, st>>>(a);
+            else narrow ? kv_scores<DT, DIM, 4, 16><<<picks, 512, 0, st>>>(a) : kv_scores<DT, DIM, 16, 16><<<picks, 512, 0, st>>>(a);
+            return hipGetLastError();
+        }
+        // as many chunks as make 1024 workgroups, of 64 to 1024 blocks
+        int64_t parts = 1024 / units;
+        if (parts < (a.width + 1023) / 1024) parts = (a.width + 1023) / 1024;
+        int64_t blocks = ((a.width + parts - 1) / parts + 63) / 64 * 64;
         while (tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) >= 1 << 24) blocks *= 2;
         a.chunk_blocks = (int)blocks;
         a.chunks = (int)((a.width + blocks - 1) / blocks);
         const unsigned groups = (unsigned)(tiles * a.kv_heads * a.chunks);
         if (a.requests) {
-            if (narrow) kv_scores<DT, DIM, 4><<<groups, 256, 0, st>>>(a);
-            else kv_scores<DT, DIM, 16><<<groups, 256, 0, st>>>(a);
+            if (narrow) kv_scores<DT, DIM, 4, 0><<<groups, 256, 0, st>>>(a);
+            else kv_scores<DT, DIM, 16, 0><<<groups, 256, 0, st>>>(a);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

@@ -93,7 +93,7 @@ struct SelectArgs {
     int32_t *selected;
     uint64_t *scores;
     int requests, row0, rows, q_heads, kv_heads, group, block_log, blocks, width, keep, first, last;
-    int tile_rows, chunks, chunk_blocks, flip;
+    int tile_rows, tiles, chunks, chunk_blocks, flip;
 };
 constexpr int kMostSelectBlocks = 32768;       // columns of the table: kv_pick holds the scores of all in registers
 size_t kv_select_workspace_bytes(const nnv_attention_desc &d, int rows);

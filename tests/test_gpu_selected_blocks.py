@@ -226,6 +226,17 @@ def test_selection_among_many_blocks(count):
         s.check_select(keep, first, last, bounds)
 
 
+@pytest.mark.parametrize("heads,lengths,fresh", [((16, 8), [8300, 3000] + [1, 40, 700, 16] * 9, [1] * 38), ((128, 8), [8300, 50], [20, 14]), ((64, 8), [600, 8300], [9, 60]),
+                                                 ((136, 8), [8300], [33])], ids=["single", "wide heads", "rows together", "seventeen heads"])
+def test_selection_in_one_launch(heads, lengths, fresh):
+    """As many rows and heads as keep the chip busy with a workgroup each."""
+    s = Scene(layer(block_tokens=16, head_dim=64, q_heads=heads[0], kv_heads=heads[1]), lengths, fresh, padding=3)
+    assert 512 < s.d.table_blocks <= 1024
+    s.positions[2] = -1
+    for keep, first, last in ((7, 1, 2), (600, 0, 0)):
+        s.check_select(keep, first, last)
+
+
 def test_selection_of_equal_scores():
     s = Scene(layer(block_tokens=16, head_dim=64), [400, 90], [3, 1])
     for value in (0.0, -0.0, 1.5):
