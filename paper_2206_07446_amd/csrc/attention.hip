@@ -381,6 +381,7 @@ template <int DIM> __device__ static inline void load_step(const AttendArgs &a, 
 }
 
 constexpr int kPartExtra = 4;      // floats of a partial result behind its values: base, sum, number of splits, whether there are any of a prefix
+constexpr int kFewestListed = 128; // of a split of a list: a round of the wavefronts (one row over 4096 tokens: 512 11.4 us, 256 10.8, 128 9.9)
 constexpr int kFewest = 512;       // tokens of a split at least, where the host knows no bound near their number
 
 // Where there is much to read (64 rows over up to 8192 tokens, 287 MB: 71 us, 4.0 TB/s; a copy moves 5.2 TB/s here, half of it reads) vector instructions take 51 % of a
@@ -457,7 +458,7 @@ template <int DT, int DIM, int SEEN, int DEPTH> __device__ static inline void at
         if (SEEN == kBoth) steps.common = steps_of<kStep>(a, seeing, uniform(row_max(own)), from, 0);
     }
     steps.sum();
-    const int each = max(steps_each(steps.count, splits), SEEN == kOwn || SEEN == kListed ? kFewest / kStep : 0), begin = split * each, end = min(steps.count, begin + each);
+    const int each = max(steps_each(steps.count, splits), SEEN == kOwn ? kFewest / kStep : SEEN == kListed ? kFewestListed / kStep : 0), begin = split * each, end = min(steps.count, begin + each);
     if (split > 0 && begin >= end) return;
     const bool whole = each >= steps.count && SEEN != kPrefix && (SEEN != kOwn || from == 0);      // no other split, or launch, has any steps
 
@@ -1327,9 +1328,10 @@ static int64_t listed_tiles(const nnv_attention_desc &d, int rows) { return (int
 int64_t kv_attention_blocks_groups(const nnv_attention_desc &d, int rows) { return listed_tiles(d, rows) * d.kv_heads; }
 
 static int listed_splits(const nnv_attention_desc &d, int rows, int keep) {
-    const int64_t groups = kv_attention_blocks_groups(d, rows), most = ((int64_t)keep * d.block_tokens + kFewest - 1) / kFewest;
+    const int64_t groups = kv_attention_blocks_groups(d, rows), most = ((int64_t)keep * d.block_tokens + kFewestListed - 1) / kFewestListed;
     const int64_t each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
-    int64_t s = (1024 + groups - 1) / groups;
+    // (64 rows and 8 heads over up to 2048 tokens: 512 workgroups 31 us, 1024 with a join 37, 2048 41)
+    int64_t s = (512 + groups - 1) / groups;
     if (s > most) s = most;
     if (s > kMostSplits) s = kMostSplits;
     while (s > 1 && (s * each > (int64_t)256 << 20 || s * groups >= 1 << 24)) s = s / 2;
