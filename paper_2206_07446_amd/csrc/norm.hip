@@ -149,9 +149,8 @@ __global__ __launch_bounds__(1024) void residual_norm(ResidualArgs a) {
 template <int XT, int YT, bool VEC> static hipError_t launch_residual_types(const ResidualArgs &args, hipStream_t st) {
     ResidualArgs a = args;
     const int eights = (a.n + 7) / 8;
-    int threads = 64;
-    while (threads < 1024 && threads < eights) threads *= 2;
-    const int chunks = (eights + threads - 1) / threads;
+    const int wanted = eights > 64 && a.m >= 512 ? 2 : 1;
+    const int each = (eights + wanted - 1) / wanted, threads = each > 1024 ? 1024 : (each + 63) / 64 * 64, chunks = (eights + threads - 1) / threads;
     a.threads = threads;
     const unsigned group = threads == 64 ? 256u : (unsigned)threads, rows = threads == 64 ? 4u : 1u, groups = (unsigned)((a.m + (int64_t)rows - 1) / rows);
     if (chunks == 1) residual_norm<XT, YT, VEC, 1><<<groups, group, 0, st>>>(a);
