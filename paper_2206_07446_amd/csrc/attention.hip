@@ -232,7 +232,9 @@ template <int R, int S> __device__ static inline Part find_part(const AttendArgs
 // Tile u of up to 63 requests with those of the longest requests first, and of each the last: every lane adds up the tiles of the
 // requests before its own.  The tiles that take longest then begin first, and the end of a launch is not theirs (4 prompts of 1024 rows over 876 to
 // 6000 tokens: see kv_attend_many).
-template <int R> __device__ static inline Tile find_longest(const AttendArgs &a, int u) {
+//
+// With a.tail the last tiles, those that would leave part of the chip idle, are cut into as many splits as fill it: u counts splits there.
+template <int R, bool TAIL> __device__ static inline Tile find_longest(const AttendArgs &a, int u, int *split, int *splits) {
     const int lane = threadIdx.x & 63;
     const bool mine = lane <= a.requests, request = lane < a.requests;
     const int start = mine ? clamped_start(a, a.starts[lane]) : a.rows, end = request ? clamped_start(a, a.starts[lane + 1]) : a.rows;
@@ -242,6 +244,17 @@ template <int R> __device__ static inline Tile find_longest(const AttendArgs &a,
     for (int j = 0; j <= a.requests; ++j) {
         const int other = __builtin_amdgcn_readlane(length, j);
         if (other > length || (other == length && j < lane)) before += __builtin_amdgcn_readlane(tiles, j);
+    }
+    if (TAIL && a.tail) {
+        int all = tiles;
+        for (int s = 1; s < 64; s *= 2) all += __shfl_xor(all, s);
+        const int last = uniform(all) % a.tail, whole = uniform(all) - last;
+        *splits = 1;
+        if (u >= whole) {
+            *splits = last ? min(max(a.tail / last, 1), a.splits) : 1;
+            *split = (u - whole) % *splits;
+            u = whole + (u - whole) / *splits;
+        }
     }
     const uint64_t found = __ballot(mine && before <= u && u < before + tiles);
     if (!found) {
@@ -724,11 +737,12 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_many_r
         split = part.split;
         splits = part.splits;
     } else {
-        const int u = rest % a.many_tiles;
-        split = rest / a.many_tiles;
+        const bool tail = SEEN == kBoth && a.tail;
+        const int u = tail ? rest : rest % a.many_tiles;
+        split = tail ? 0 : rest / a.many_tiles;
         splits = a.splits;
         if (a.ordered) {
-            t = find_longest<kManyRows>(a, u);
+            t = find_longest<kManyRows, SEEN == kBoth>(a, u, &split, &splits);
             if ((SEEN == kOwn || SEEN == kBoth) && t.pairs > 0 && t.request < a.requests) {
                 if (t.request_pairs < kManyPairs) return;
                 prefix = request_prefix(a, t.request);
@@ -973,7 +987,7 @@ template <int DT, int DIM, int SEEN> __device__ static inline void attend_many_r
                 *reinterpret_cast<f32x4_t *>(parts + at) = f32x4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
             }
         }
-    if ((splits > 1 || SEEN == kPrefix || SEEN == kOwn) && half == 0) {
+    if ((a.splits > 1 || SEEN == kPrefix || SEEN == kOwn) && half == 0) {
         parts[DIM] = base;
         parts[DIM + 1] = sum;
         parts[DIM + 2] = __builtin_bit_cast(float, whole || steps.count == 0 ? 1 : (steps.count + each - 1) / each);
@@ -1103,13 +1117,11 @@ __global__ __launch_bounds__(256) void kv_attend_join_shared(AttendArgs a) {
 }
 
 // The same with a wavefront to a row and query head, where there are many of these: nothing waits for another, and a wavefront's loads are all on their way.
-template <int DT, int DIM>
-__global__ __launch_bounds__(256) void kv_attend_join_rows(AttendArgs a, int all) {
+template <int DT, int DIM> __device__ static inline void join_row(const AttendArgs &a, int row) {
     typedef typename Elem<DT>::type T;
     constexpr int kEach = DIM / 64;
     typedef float FV __attribute__((ext_vector_type(kEach)));
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
-    if (row >= all) return;
+    const int lane = threadIdx.x & 63;
     const float *p = a.parts + (int64_t)row * a.slots * (DIM + kPartExtra), *own = p + a.prefix_splits * (DIM + kPartExtra);
     // (a lane to a slot, and one more slot each where there are more than 64; what is read of results that there are not is not used)
     float bases[4], sums[4], m = -3.4028234663852886e38f, l = 0;
@@ -1159,6 +1171,21 @@ __global__ __launch_bounds__(256) void kv_attend_join_rows(AttendArgs a, int all
     for (int i = 0; i < kEach; ++i) y[i] = (T)(l == 0 ? 0.f : v[i] / l);
     *reinterpret_cast<ElemVec<DT, kEach> *>(static_cast<T *>(a.out) + (int64_t)row * DIM + kEach * lane) = y;
 }
+template <int DT, int DIM>
+__global__ __launch_bounds__(256) void kv_attend_join_rows(AttendArgs a, int all) {
+    const int row = blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    if (row < all) join_row<DT, DIM>(a, row);
+}
+// Of two rows and query heads a wavefront, those that have more than one part.  (16 prompts behind a prefix, 72600 of them, a seventh with parts: the whole call
+// 203 us, with one a wavefront 208, with 4 205, 8 212, 16 224.)
+constexpr int kJoinRows = 2;
+template <int DT, int DIM>
+__global__ __launch_bounds__(256) void kv_attend_join_some(AttendArgs a, int all) {
+    const int lane = threadIdx.x & 63, first = (blockIdx.x * 4 + uniform(threadIdx.x >> 6)) * kJoinRows;
+    const bool mine = lane < kJoinRows && first + lane < all;
+    const int parts = mine ? __builtin_bit_cast(int, a.parts[(int64_t)(first + lane) * a.slots * (DIM + kPartExtra) + DIM + 2]) : 0;
+    for (uint64_t left = __ballot(parts > 1); left; left &= left - 1) join_row<DT, DIM>(a, first + __builtin_ctzll(left));
+}
 
 static int attend_tiles(int requests, int rows, int group, int tile) { return (int)(((int64_t)rows * group) / tile) + requests + 1; }
 
@@ -1201,19 +1228,24 @@ size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, i
 
 template <int DT, int DIM, int SEEN> static hipError_t launch_attend_dim(const AttendArgs &a, hipStream_t st) {
     if (a.many) {
-        kv_attend_many<DT, DIM, SEEN><<<(unsigned)(a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
+        kv_attend_many<DT, DIM, SEEN><<<(unsigned)(a.tail ? (a.many_tiles + a.tail) * a.kv_heads : a.many_tiles * a.kv_heads * a.splits), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (a.tiles) kv_attend<DT, DIM, SEEN><<<(unsigned)(a.tiles * a.kv_heads * a.splits), 64 * kAttendWaves, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
+    const int all = a.rows * a.q_heads;
+    if (a.tail) kv_attend_join_some<DT, DIM><<<(unsigned)((all + 4 * kJoinRows - 1) / (4 * kJoinRows)), 256, 0, st>>>(a, all);
+    else kv_attend_join<DT, DIM><<<(unsigned)(a.rows * a.q_heads), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 template <int DT> static hipError_t launch_attend_type(const AttendArgs &a, int dim, hipStream_t st) {
     return dim == 64 ? launch_attend_dim<DT, 64, kAll>(a, st) : dim == 128 ? launch_attend_dim<DT, 128, kAll>(a, st) : launch_attend_dim<DT, 256, kAll>(a, st);
 }
+
+// The order costs a loop over the requests, and is for tiles that take many steps.
+static bool longest_first(const nnv_attention_desc &d, int requests) { return requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024; }
 
 static AttendArgs with_sizes(const nnv_attention_desc &d, const AttendArgs &args) {
     AttendArgs a = args;
@@ -1222,8 +1254,7 @@ static AttendArgs with_sizes(const nnv_attention_desc &d, const AttendArgs &args
     a.many_tiles = attend_tiles(a.requests, a.rows, a.group, kManyRows);
     a.splits = attend_splits(d, a.requests, a.rows);
     a.group_inverse = ((1u << 21) + a.group - 1) / a.group;
-    // the order costs a loop over the requests, and is for tiles that take many steps
-    a.ordered = a.requests < 64 && (int64_t)d.table_blocks * d.block_tokens > 1024;
+    a.ordered = longest_first(d, a.requests);
     return a;
 }
 
@@ -1236,8 +1267,16 @@ hipError_t launch_kv_attention(const nnv_attention_desc &d, const AttendArgs &ar
 // ---- a prefix read once for the requests that share it, and what each has behind it ------------------------------------------
 
 // Where requests have 256 pairs and more on average, their tiles go over the prefix by themselves: it is converted for 128 pairs at a time either way, and nothing is to
-// be joined (16 requests of up to 256 rows behind 4096 tokens, 32 heads: ... us, in two parts 328).
+// be joined (16 requests of up to 256 rows behind 4096 tokens, 32 heads of 128 and 8 of keys: 230 us, in two parts 328).
 static bool shared_by_request(const nnv_attention_desc &d, int requests, int rows) { return (int64_t)rows * (d.q_heads / d.kv_heads) >= (int64_t)2 * kManyRows * requests; }
+
+// Of these, where the longest go first, how many splits the tiles have that are left when the chip has been filled for the last time: 2 to 8 within 128 MB of partial
+// results; 0: tiles are cut alike, if at all.
+static int tail_splits(const nnv_attention_desc &d, int requests, int rows) {
+    if (!shared_by_request(d, requests, rows) || !attend_many(d, requests, rows) || !longest_first(d, requests) || d.kv_heads > 64) return 0;
+    const int64_t fit = ((int64_t)128 << 20) / ((int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4);
+    return fit < 2 || 8 * kv_attention_groups(d, requests, rows) >= 1 << 24 ? 0 : fit < 8 ? (int)fit : 8;
+}
 
 // Otherwise prefixes and what is behind them are two parts, whose results are joined.  The prefix goes by 128 pairs, converted once for them, where a group has as
 // many on average as fill a wavefront's part of those.
@@ -1285,13 +1324,20 @@ int64_t kv_attention_shared_groups(const nnv_attention_desc &d, int requests, in
 }
 
 size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    if (const int s = tail_splits(d, requests, rows)) return (size_t)rows * d.q_heads * s * (d.head_dim + kPartExtra) * 4;
     if (shared_by_request(d, requests, rows)) return kv_attention_workspace_bytes(d, requests, rows);
     return (size_t)rows * d.q_heads * shared_sizes(d, requests, rows, groups).slots * (d.head_dim + kPartExtra) * 4;
 }
 
 template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attention_desc &d, const AttendArgs &args, hipStream_t st) {
     AttendArgs a = with_sizes(d, args);
-    if (shared_by_request(d, a.requests, a.rows)) return launch_attend_dim<DT, DIM, kBoth>(a, st);
+    if (shared_by_request(d, a.requests, a.rows)) {
+        if (const int splits = tail_splits(d, a.requests, a.rows)) {
+            a.splits = a.slots = splits;
+            a.tail = (d.head_dim == 64 ? 768 : d.head_dim == 128 ? 512 : 256) / a.kv_heads;
+        }
+        return launch_attend_dim<DT, DIM, kBoth>(a, st);
+    }
     const SharedSizes s = shared_sizes(d, a.requests, a.rows, a.n_groups);
     a.slots = s.slots;
     a.prefix_splits = s.prefix;

@@ -99,6 +99,21 @@ class Shared:
         return got
 
 
+    def check_rows(self, got, rows):
+        """Some rows only."""
+        d, half = self.d, self.d.dtype == nnv.F16
+        u = torch.finfo(T[d.dtype]).eps / 2
+        for r in rows:
+            i = int(np.searchsorted(self.starts, r, "right")) - 1
+            if i >= len(self.lengths):
+                assert (got[r] == 0).all()
+                continue
+            k, v = OS.round_head(self.k[i].double().numpy(), half), OS.round_head(self.v[i].double().numpy(), half)
+            ref, size, most = OS.attention(self.q[r:r + 1].double().numpy(), k, v, self.positions[r:r + 1], d.scale, d.window, d.sinks)
+            bound = (u + 2 * OS.score_bound(d.head_dim, most) + (len(k) + 64) * 2.0 ** -23) * size * (1 + 2.0 ** -6) + u * (1 + 2.0 ** -6) * np.abs(ref) + float(torch.finfo(T[d.dtype]).tiny)
+            assert (np.abs(got[r] - ref[0]) <= bound[0]).all(), f"row {r} of request {i}"
+
+
 SCENES = [([1], [[1]], 1), ([16], [[1, 5, 40]], 1), ([100], [[3, 3, 50, 16]], 1), ([65, 33], [[2, 80], [1, 1, 1]], 1), ([200, 7, 64], [[1], [30, 2], [64, 65, 1, 1]], 2)]
 
 
@@ -123,6 +138,26 @@ def test_prompts_behind_a_prefix(dim, dtype):
     for block in (16, 128):
         d = layer(head_dim=dim, q_heads=16, kv_heads=1, block_tokens=block, dtype=dtype, scale=dim ** -0.5)
         Shared(d, [150, 64], [[70, 3, 40], [100, 1]], [70, 3, 40, 100, 1], padding=3).check()
+
+
+@pytest.mark.parametrize("dim,heads", [(64, (32, 2)), (128, (64, 8)), (256, (48, 4))], ids=str)
+def test_prompts_whose_last_tiles_are_split(dim, heads):
+    """Tiles of 128 pairs that fill the chip less than once, and once and a part; requests of a row or two beside them."""
+    for members in ([[90, 1, 130, 64], [200, 3]], [[500, 1, 700, 300], [2, 450]]):
+        rows = [min(n, 400) for m in members for n in m]
+        s = Shared(layer(head_dim=dim, q_heads=heads[0], kv_heads=heads[1], block_tokens=32, dtype=nnv.F16 if dim == 64 else nnv.BF16, scale=dim ** -0.5), [1100, 333], members,
+                   [0 if n == 3 else n for n in rows], padding=2)
+        few = list(range(0, s.rows, 1 + s.rows // 60))
+        got = s.run()
+        assert np.array_equal(got, s.run())
+        s.check_rows(got, few)
+
+
+@pytest.mark.parametrize("heads,dim", [((16, 1), 64), ((40, 2), 128), ((16, 2), 256)], ids=str)
+def test_requests_of_some_rows_each(heads, dim):
+    """Own tokens of 32 to 255 pairs a request by 128 pairs, beside prefixes that all share."""
+    s = Shared(layer(q_heads=heads[0], kv_heads=heads[1], block_tokens=16, head_dim=dim, scale=dim ** -0.5), [150, 70], [[9, 30, 2, 77] * 6, [40, 8] * 5], [7, 3, 1, 9, 4, 12] * 6, padding=1)
+    s.check()
 
 
 @pytest.mark.parametrize("fresh", [[60, 9, 12], [30, 1, 1]], ids=str)
