@@ -1294,15 +1294,15 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
         return (int)(splits < 1 ? 1 : splits);
     };
     const int64_t tile = s.many ? kManyRows : kTileRows, prefix_tiles = pairs / tile + groups + 1;
-    if (groups) {
-        const int64_t target = 384;
-        s.units = (int)((target + d.kv_heads - 1) / d.kv_heads);
-        s.least = s.many ? 8 : 4;
-        if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
-        else s.prefix = within(s.units, capacity / 128 + 1);
-        // (parts are no more than units where tiles are no more than half of those: see find_part)
-        s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : prefix_tiles <= s.units / 2 ? s.units : s.units + prefix_tiles) * d.kv_heads;
-    }
+    // 384 workgroups for prefixes: the chip holds 512 of these, and the others' places are for what is behind (96 requests behind five prefixes of up to 16001
+    // tokens: 256 140 us, 320 132, 384 115, 448 117, 512 120); parts of 512 tokens at least by 128 pairs (64 requests behind 8192 tokens: 256 51 us, 512 42), one
+    // round of the wavefronts by 16.
+    s.units = (384 + d.kv_heads - 1) / d.kv_heads;
+    s.least = s.many ? 8 : 4;
+    if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
+    else s.prefix = within(s.units, capacity / 128 + 1);
+    // (parts are no more than units where tiles are no more than half of those: see find_part)
+    s.prefix_groups = (groups > 64 ? prefix_tiles * s.prefix : prefix_tiles <= s.units / 2 ? s.units : s.units + prefix_tiles) * d.kv_heads;
     const int64_t own_tile = own_many ? kManyRows : kTileRows, full = pairs / own_tile, least = requests < rows ? requests : rows;
     const int64_t own_tiles = (full > least ? full : least > 0 ? least : 1) * d.kv_heads;
     s.own = within((512 + own_tiles - 1) / own_tiles, capacity / kFewest + 1);
@@ -1318,12 +1318,14 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
 }
 
 int64_t kv_attention_shared_groups(const nnv_attention_desc &d, int requests, int rows, int groups) {
-    if (shared_by_request(d, requests, rows)) return kv_attention_groups(d, requests, rows);
+    if (!groups || shared_by_request(d, requests, rows)) return kv_attention_groups(d, requests, rows);
     const SharedSizes s = shared_sizes(d, requests, rows, groups);
-    return s.prefix_groups + s.own_many + s.own_few;
+    const int64_t all = s.prefix_groups + s.own_many + s.own_few, join = ((int64_t)rows * d.q_heads + 3) / 4;
+    return all > join ? all : join;
 }
 
 size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requests, int rows, int groups) {
+    if (!groups) return kv_attention_workspace_bytes(d, requests, rows);
     if (const int s = tail_splits(d, requests, rows)) return (size_t)rows * d.q_heads * s * (d.head_dim + kPartExtra) * 4;
     if (shared_by_request(d, requests, rows)) return kv_attention_workspace_bytes(d, requests, rows);
     return (size_t)rows * d.q_heads * shared_sizes(d, requests, rows, groups).slots * (d.head_dim + kPartExtra) * 4;
@@ -1331,6 +1333,7 @@ size_t kv_attention_shared_workspace_bytes(const nnv_attention_desc &d, int requ
 
 template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attention_desc &d, const AttendArgs &args, hipStream_t st) {
     AttendArgs a = with_sizes(d, args);
+    if (!a.n_groups) return launch_attend_dim<DT, DIM, kAll>(a, st);
     if (shared_by_request(d, a.requests, a.rows)) {
         if (const int splits = tail_splits(d, a.requests, a.rows)) {
             a.splits = a.slots = splits;

@@ -531,7 +531,7 @@ template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs 
             return hipGetLastError();
         }
         // as many chunks as make 1024 workgroups, of 64 to 1024 blocks
-        int64_t parts = 1024 / units;
+        int64_t parts = 1024 / (units ? units : 1);      // (without requests there is no tile)
         if (parts < (a.width + 1023) / 1024) parts = (a.width + 1023) / 1024;
         int64_t blocks = ((a.width + parts - 1) / parts + 63) / 64 * 64;
         while (tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) >= 1 << 24) blocks *= 2;

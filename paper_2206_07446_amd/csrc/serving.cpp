@@ -17,7 +17,7 @@ inline int finish(hipError_t e) { return e == hipSuccess ? NNV_OK : record_hip_e
 // Sizes that the kernels' grids can hold.
 constexpr int kMostLinearN = 1 << 22, kMostLinearK = 1 << 20, kMostLinearRows = 65535 * 16;
 constexpr int kMostRows = 1 << 24, kMostRequests = 1 << 20;
-constexpr int kMostResidual = 32768, kMostResidualRows = 1 << 22;      // (1024 threads a row: fewer than 2^32)
+constexpr int kMostResidual = 32768, kMostResidualRows = (1 << 22) - 1;      // (1024 threads a row: fewer than 2^32)
 constexpr int kMostKeep = 1 << 20;                     // (its tokens are counted in 32 bits)
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 constexpr int64_t kMostGroups = (1 << 24) - 1;        // workgroups of 256: a launch has fewer than 2^32 threads
@@ -99,7 +99,7 @@ int check_selecting(const nnv_attention_desc *d) {
 
 // More workgroups than a launch can have, of either kernel of a selection, at the fewest that a size can be cut into.
 bool select_too_large(const nnv_attention_desc &d, int requests, int rows) {
-    return ((int64_t)rows + requests) * d.kv_heads > (int64_t)1 << 22;      // (1024 threads a row and key head)
+    return ((int64_t)rows + requests) * d.kv_heads >= (int64_t)1 << 22;     // (1024 threads a row and key head)
 }
 
 // What an attention call takes, checked; out and the workspace lie apart from the inputs and each other.

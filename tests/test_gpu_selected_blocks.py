@@ -356,6 +356,21 @@ def test_attention_where_blocks_are_none():
     assert (got[1] == 0).all() and (got[4:] == 0).all()
 
 
+def test_rows_without_any_request():
+    d = layer(block_tokens=16, head_dim=64)
+    ws = torch.full((1 << 20,), 0xFF, dtype=torch.uint8, device=DEV)
+    cache = torch.zeros(nnv.nnv_kv_cache_bytes(d), dtype=torch.uint8, device=DEV)
+    bounds = torch.zeros(nnv.nnv_kv_bounds_bytes(d), dtype=torch.uint8, device=DEV)
+    q, out = torch.ones(3, 8, 64, dtype=torch.bfloat16, device=DEV), torch.full((3, 8, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    selected = torch.full((3, 2, 4), 7, dtype=torch.int32, device=DEV)
+    none, starts, positions = None, ints([0]), ints([5, 0, -1])
+    nnv.nnv_kv_bounds(d, 0, 3, none, starts, none, cache, bounds)
+    nnv.nnv_kv_select(d, 0, 3, 4, 1, 1, q, none, starts, none, positions, bounds, selected, ws)
+    nnv.nnv_kv_attention_blocks(d, 0, 3, 4, q, none, starts, none, positions, selected, cache, out, ws)
+    torch.cuda.synchronize()
+    assert (selected == -1).all() and (out == 0).all()
+
+
 def test_all_blocks_are_attention():
     """Lists of all that a row sees: the definition of attention over the whole cache."""
     for fresh in ([1, 1], [70, 5]):

@@ -183,6 +183,24 @@ def test_requests_of_no_group():
     s.check()
 
 
+def test_no_groups_and_no_requests():
+    """Without groups the call is attention over the cache, byte by byte; without requests rows are zeros."""
+    for fresh in (1, 60):
+        s = Shared(layer(block_tokens=16), [], [], fresh, loose=[7, 90, 700], padding=1)
+        n, out = len(s.lengths), torch.zeros(s.rows, 8, 128, dtype=torch.bfloat16, device=DEV)
+        ws = torch.zeros(nnv.nnv_kv_attention_workspace_bytes(s.d, n, s.rows) + 16, dtype=torch.uint8, device=DEV)
+        nnv.nnv_kv_attention(s.d, n, s.rows, s.q.to(DEV), ints(s.table), ints(s.starts), ints(s.lengths), ints(s.positions), s.cache, out, ws)
+        torch.cuda.synchronize()
+        assert np.array_equal(s.run(n_groups=0), out.double().cpu().numpy())
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    out = torch.full((3, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    for groups in (0, 2):
+        out.fill_(7)
+        nnv.nnv_kv_attention_shared(s.d, 0, 3, groups, s.q[:3].to(DEV), None, ints([0]), None, ints([5, 0, -1]), ints([0, 0, 0]), ints([9, 9]), s.cache, out, ws)
+        torch.cuda.synchronize()
+        assert (out == 0).all()
+
+
 def test_prefixes_of_nothing_and_of_more_than_is_held():
     s = Shared(layer(block_tokens=16), [0], [[30, 200]], 1)
     s.check()

@@ -128,6 +128,11 @@ def test_workspaces(calls):
     # scores of many rows are kept for some of them at a time
     assert nnv.nnv_kv_select_workspace_bytes(layer(table_blocks=32768), 3, 1 << 20) <= 256 << 20
     assert nnv.nnv_kv_select_workspace_bytes(layer(), 3, 1 << 22) == 0
+    assert nnv.nnv_kv_select_workspace_bytes(layer(), 0, 1 << 21) == 0                           # 2^32 threads of 1024 a row and head
+    # a wavefront joins each row and query head: no more of these than a launch has
+    wide = layer(q_heads=1024, kv_heads=64)
+    assert nnv.nnv_kv_attention_shared_workspace_bytes(wide, 1 << 16, 1 << 16, 1) == 0
+    assert status(nnv.nnv_kv_attention_shared, wide, 1 << 16, 1 << 16, 1, *apart(10), BIG) == ARG
     fn, args, _, _ = args_of("select", (1, 1 << 22, 4, 1, 2))
     assert status(fn, layer(), *args) == ARG
     many = layer(q_heads=1024, kv_heads=1)
@@ -156,7 +161,7 @@ def test_residual_descriptors(calls, bad):
 
 def test_residual_refusals(calls):
     d, f = residual(), nnv.nnv_residual_norm
-    for kw in (dict(m=-1), dict(m=(1 << 22) + 1), dict(ldx=95), dict(ldy=95), dict(ldo=95), dict(ldh=95), dict(ldg=95), dict(gates=0), dict(gates=2, index=None),
+    for kw in (dict(m=-1), dict(m=1 << 22), dict(ldx=95), dict(ldy=95), dict(ldo=95), dict(ldh=95), dict(ldg=95), dict(gates=0), dict(gates=2, index=None),
                dict(ldx=(1 << 40) + 1)):
         assert status(f, d, *residual_args(**kw)) == ARG, kw
     for name in ("x", "x_out", "h"):
