@@ -4,7 +4,8 @@
 // r = x + scale * gate * (y / sqrt(mean(y^2) + eps) * post),  h = r / sqrt(mean(r^2) + eps) * pre
 //
 // A row stays in the registers of the threads that read it, so that each input is read once and each output written once: bound by that traffic, and for a
-// few rows by the chain of loads, two sums over the row and the stores.
+// few rows by the chain of loads, two sums over the row and the stores.  8191 rows of 5120 (float32 stream, gates, both norms, 503 MB): 99 us, 5.1 TB/s, the rate of a
+// copy; 64 rows of 4096: 4.2 us.
 #include <type_traits>
 #include "nnv_internal.h"
 #include "serving.h"
@@ -149,6 +150,7 @@ __global__ __launch_bounds__(1024) void residual_norm(ResidualArgs a) {
 template <int XT, int YT, bool VEC> static hipError_t launch_residual_types(const ResidualArgs &args, hipStream_t st) {
     ResidualArgs a = args;
     const int eights = (a.n + 7) / 8;
+    // (two loads of eight a thread where there are many rows: 8191 rows of 5120 99 us, with one 103, with four 151, spilt; 1024 threads for the 640 that have work 107)
     const int wanted = eights > 64 && a.m >= 512 ? 2 : 1;
     const int each = (eights + wanted - 1) / wanted, threads = each > 1024 ? 1024 : (each + 63) / 64 * 64, chunks = (eights + threads - 1) / threads;
     a.threads = threads;
