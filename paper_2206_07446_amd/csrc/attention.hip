@@ -207,9 +207,11 @@ template <int R, int S> __device__ static inline Part find_part(const AttendArgs
     // (each tile's last part counts as one more; rounded up by more than the sum is off: no more parts than there are workgroups)
     const float units = fmaxf(a.prefix_units - whole, 0.5f * a.prefix_units);
     int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / units), 1e9f));
+    // (where that would be less than prefix_short, two thirds of the parts: what a part costs beside its steps is then most of it)
+    auto shortest_of = [&](float length) { return length < a.prefix_short ? min(max((int)ceilf(length * 1.5f), a.prefix_least), a.prefix_short) : (int)fminf(ceilf(length), 1e9f); };
     if (a.n_groups <= 16) {
         // of 64 lengths from the shortest that could do, a lane each, the first that gives no more parts than that
-        const int shortest = max(a.prefix_least, (int)fminf(ceilf(total / a.prefix_units), 1e9f)), tried = shortest + lane * ((shortest + 63) / 64);
+        const int shortest = max(a.prefix_least, shortest_of(total / a.prefix_units)), tried = shortest + lane * ((shortest + 63) / 64);
         float parts = 0;
         for (int g = 0; g < a.n_groups; ++g)
             parts += (float)__builtin_amdgcn_readlane(tiles, g) * (float)min((__builtin_amdgcn_readlane(steps, g) + tried - 1) / tried, a.prefix_splits);
@@ -1287,7 +1289,7 @@ struct SharedSizes { bool many; int units, least, prefix, own, slots; int64_t pr
 static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int rows, int groups) {
     const int group = d.q_heads / d.kv_heads;
     const int64_t capacity = (int64_t)d.table_blocks * d.block_tokens, pairs = (int64_t)rows * group, each = (int64_t)rows * d.q_heads * (d.head_dim + kPartExtra) * 4;
-    const bool own_many = attend_many(d, requests, rows) && pairs >= (int64_t)kManyPairs * requests;      // (of fewer on average, nearly all are few)
+    const bool own_many = attend_many(d, requests, rows) && pairs >= (int64_t)2 * kManyPairs * requests;      // (of fewer on average, nearly all are few)
     SharedSizes s{};
     s.many = own_many || pairs >= (int64_t)kManyPairs * groups;
     auto within = [&](int64_t splits, int64_t most) {     // of memory, and of what the join takes
@@ -1298,10 +1300,11 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
     };
     const int64_t tile = s.many ? kManyRows : kTileRows, prefix_tiles = pairs / tile + groups + 1;
     // 384 workgroups for prefixes: the chip holds 512 of these, and the others' places are for what is behind (96 requests behind five prefixes of up to 16001
-    // tokens: 256 140 us, 320 132, 384 115, 448 117, 512 120); parts of 512 tokens at least by 128 pairs (64 requests behind 8192 tokens: 256 51 us, 512 42), one
-    // round of the wavefronts by 16.
+    // tokens: 256 140 us, 320 132, 384 115, 448 117, 512 120); 256 where parts are short
+    // (64 requests behind 8192 tokens: parts of 256 tokens 51 us, of 512 42; the other way round 191 requests of 3 rows behind up to 481 tokens and heads of 256: parts of 128
+    // tokens 30 us, of 512 43); by 16 pairs a round of the wavefronts at least.
     s.units = (384 + d.kv_heads - 1) / d.kv_heads;
-    s.least = s.many ? 8 : 4;
+    s.least = s.many && d.head_dim == 256 ? 2 : 4;
     if (groups > 64) s.prefix = within((s.units + prefix_tiles - 1) / prefix_tiles, capacity / kFewest + 1);
     else s.prefix = within(s.units, capacity / 128 + 1);
     // (parts are no more than units where tiles are no more than half of those: see find_part)
@@ -1349,14 +1352,28 @@ template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attenti
     a.prefix_splits = s.prefix;
     a.prefix_units = s.units;
     a.prefix_least = s.least;
+    a.prefix_short = s.many ? 8 : 4;
     a.prefix_groups = (int)s.prefix_groups;
     a.own_many = (int)s.own_many;
     a.many = s.own_many > 0;
     a.tiles = (int)(s.own_few / ((int64_t)a.kv_heads * s.own));
     a.splits = s.own;
     const unsigned groups = (unsigned)(s.prefix_groups + s.own_many + s.own_few);
-    if (s.many) kv_attend_shared<DT, DIM, true><<<groups, 256, 0, st>>>(a);
-    else kv_attend_shared<DT, DIM, false><<<groups, 256, 0, st>>>(a);
+    if (!s.many) {
+        kv_attend_shared<DT, DIM, false><<<groups, 256, 0, st>>>(a);
+    } else if constexpr (DIM == 256) {
+        // heads of 256 leave room for one workgroup of these a compute unit, and the others would have no more: a launch each (114 requests of a token behind 164, 16 heads
+        // to a key head: in one launch 64 us, in these 54)
+        kv_attend_many<DT, DIM, kPrefix><<<(unsigned)s.prefix_groups, 256, 0, st>>>(a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (s.own_many) kv_attend_many<DT, DIM, kOwn><<<(unsigned)s.own_many, 256, 0, st>>>(a);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        kv_attend<DT, DIM, kOwn><<<(unsigned)s.own_few, 64 * kAttendWaves, 0, st>>>(a);
+    } else {
+        kv_attend_shared<DT, DIM, true><<<groups, 256, 0, st>>>(a);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int all = a.rows * a.q_heads;

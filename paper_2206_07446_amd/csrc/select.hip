@@ -502,6 +502,20 @@ __global__ __launch_bounds__(THREADS) void kv_pick(SelectArgs a) {
     for (int i = chosen + t; i < a.keep; i += THREADS) out[i] = -1;
 }
 
+// The same with a wavefront to a row and head, where there are many: nothing waits for another at every bit.
+template <int EACH>
+__global__ __launch_bounds__(256) void kv_pick_rows(SelectArgs a) {
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= (int64_t)a.rows * a.kv_heads) return;
+    const int row = a.row0 + (int)(unit / a.kv_heads), head = (int)(unit % a.kv_heads);
+    const int position = a.positions[row];
+    Found f{};
+    if (a.requests) f = last_place(a.requests, row, a.lengths, [&](int i) { return a.starts[i]; }, [](int, int start) { return (int64_t)start; });
+    const int length = f.start <= row && row < f.end ? min(max(f.length, 0), a.width << a.block_log) : 0;
+    const int last = min(position, length - 1), visible = last < 0 ? 0 : (last >> a.block_log) + 1;
+    pick_by_wave<EACH>(a.scores + unit * a.width, visible, a.first, a.last, a.keep, a.selected + ((int64_t)row * a.kv_heads + head) * a.keep);
+}
+
 constexpr int64_t kScoreBytes = (int64_t)256 << 20;
 
 // Rows whose scores are kept at a time.
@@ -534,8 +548,9 @@ template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs 
             else narrow ? kv_scores<DT, DIM, 4, 16><<<picks, 512, 0, st>>>(a) : kv_scores<DT, DIM, 16, 16><<<picks, 512, 0, st>>>(a);
             return hipGetLastError();
         }
-        // as many chunks as make 1024 workgroups, of 64 to 1024 blocks
-        int64_t parts = 1024 / (units ? units : 1);      // (without requests there is no tile)
+        // as many chunks as make 1536 workgroups, of 64 to 1024 blocks, by the tiles that there are at least
+        const int64_t whole = a.rows / a.tile_rows, least = a.requests < a.rows ? a.requests : a.rows, there = (whole > least ? whole : least) * a.kv_heads;
+        int64_t parts = 1536 / (there ? there : 1);
         if (parts < (a.width + 1023) / 1024) parts = (a.width + 1023) / 1024;
         int64_t blocks = ((a.width + parts - 1) / parts + 63) / 64 * 64;
         while (tiles * a.kv_heads * ((a.width + blocks - 1) / blocks) >= 1 << 24) blocks *= 2;
@@ -549,7 +564,14 @@ template <int DT, int DIM> static hipError_t launch_select_dim(const SelectArgs 
             if (e != hipSuccess) return e;
         }
         const unsigned picks = (unsigned)a.rows * a.kv_heads;
-        if (a.width <= 512) kv_pick<64, 8><<<picks, 64, 0, st>>>(a);
+        // (4775 rows and heads over up to 788 blocks: workgroups of 256 33 us, a wavefront each 24; 1612 over up to 2233: of 1024 60, 40)
+        if (picks >= 512 && a.width <= 4096) {
+            const unsigned fours = (picks + 3) / 4;
+            if (a.width <= 512) kv_pick_rows<8><<<fours, 256, 0, st>>>(a);
+            else if (a.width <= 1024) kv_pick_rows<16><<<fours, 256, 0, st>>>(a);
+            else if (a.width <= 2048) kv_pick_rows<32><<<fours, 256, 0, st>>>(a);
+            else kv_pick_rows<64><<<fours, 256, 0, st>>>(a);
+        } else if (a.width <= 512) kv_pick<64, 8><<<picks, 64, 0, st>>>(a);
         else if (a.width <= 2048) kv_pick<256, 8><<<picks, 256, 0, st>>>(a);
         else if (a.width <= 8192) kv_pick<1024, 8><<<picks, 1024, 0, st>>>(a);
         else kv_pick<1024, 32><<<picks, 1024, 0, st>>>(a);

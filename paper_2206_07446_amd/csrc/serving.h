@@ -67,7 +67,7 @@ struct AttendArgs {
     // nnv_kv_attention_shared: partial results of a row and query head, the most splits of a prefix (their results come first), workgroups that prefixes are cut into (of a
     // key head) and the fewest steps of one, launched workgroups of prefixes and of requests of many rows
     int tail;                                  // workgroups of a key head that the chip holds: tiles that do not fill it once more are split (0: none are)
-    int slots, prefix_splits, prefix_units, prefix_least, prefix_groups, own_many;
+    int slots, prefix_splits, prefix_units, prefix_least, prefix_short, prefix_groups, own_many;
 };
 int64_t kv_attention_groups(const nnv_attention_desc &d, int requests, int rows);     // tiles of rows times key/value heads
 size_t kv_attention_workspace_bytes(const nnv_attention_desc &d, int requests, int rows);

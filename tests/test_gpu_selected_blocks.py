@@ -237,6 +237,19 @@ def test_selection_in_one_launch(heads, lengths, fresh):
         s.check_select(keep, first, last)
 
 
+@pytest.mark.parametrize("count", [300, 513, 1025, 2049])
+def test_selection_of_many_rows_among_many_blocks(count):
+    """A wavefront to a row and head, for each number of keys that its lanes hold; bounds of a few values, so that many scores are equal."""
+    s = Scene(layer(block_tokens=16, head_dim=64, q_heads=8, kv_heads=8), [count * 16 - 5, 100], [66, 3], padding=1)
+    g = torch.Generator().manual_seed(count)
+    pool = torch.sort(torch.randint(-2, 3, (200, 8, 2, 64), generator=g).to(torch.bfloat16), 2, descending=True).values
+    bounds = pool[torch.randint(200, (s.d.blocks,), generator=g)].contiguous().to(DEV)
+    s.positions[4] = -1
+    s.table[0][3] = -1
+    for keep, first, last in ((9, 1, 2), (count - 2, 0, 1)):
+        s.check_select(keep, first, last, bounds)
+
+
 def test_selection_of_equal_scores():
     s = Scene(layer(block_tokens=16, head_dim=64), [400, 90], [3, 1])
     for value in (0.0, -0.0, 1.5):
