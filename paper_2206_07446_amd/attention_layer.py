@@ -9,6 +9,7 @@ stream to the residual stream and the norm for the next layer.
 from __future__ import annotations
 
 import argparse
+import math
 
 import torch
 
@@ -155,11 +156,18 @@ class AttentionLayer:
         if not (isinstance(x, torch.Tensor) and x.dtype in types and x.device == self.qkv.device and x.dim() == 2 and x.shape[0] >= rows and x.shape[1] == self.hidden
                 and x.stride(1) == 1 and (rows <= 1 or x.stride(0) >= self.hidden) and x.data_ptr() % 16 == 0):
             raise ValueError(f"expected a stream of {rows} rows or more of {self.hidden} values on {self.qkv.device}, each without gaps, the first 16-byte aligned")
-        gates, stride = (0, 0) if gate is None else (gate.shape[0], gate.stride(0))
-        if gate is not None and not (gate.dtype == self.dtype and gate.device == self.qkv.device and gate.dim() == 2 and gate.shape[1] == self.hidden and gate.stride(1) == 1):
-            raise ValueError(f"expected gates of {self.hidden} {self.dtype} on {self.qkv.device}")
-        if index is not None and not (index.dtype == torch.int32 and index.device == self.qkv.device and index.is_contiguous() and index.numel() >= rows):
+        gates, stride = (0, 0) if gate is None or gate.dim() != 2 else (gate.shape[0], gate.stride(0))
+        if gate is not None and not (isinstance(gate, torch.Tensor) and gate.dtype == self.dtype and gate.device == self.qkv.device and gate.dim() == 2 and gates >= 1
+                                     and gate.shape[1] == self.hidden and gate.stride(1) == 1 and (gates == 1 or stride >= self.hidden) and gate.data_ptr() % 16 == 0
+                                     and (index is not None or gates == 1 or gates >= rows)):
+            raise ValueError(f"expected gates of {self.hidden} {self.dtype} on {self.qkv.device}, one, {rows} or an index for each row")
+        if not math.isfinite(scale):
+            raise ValueError("expected a finite scale")
+        if index is not None and not (isinstance(index, torch.Tensor) and index.dtype == torch.int32 and index.device == self.qkv.device and index.is_contiguous() and index.numel() >= rows):
             raise ValueError(f"expected {rows} int32 or more on {self.qkv.device}")
+        memory = [t.untyped_storage().data_ptr() for t in (x, h, gate, index) if t is not None]      # (what is written, first)
+        if rows and (memory[0] in memory[1:] or memory[1] in memory[2:]):
+            raise ValueError("expected the stream and the norms in memory of their own")
         desc = nnv.ResidualDesc(n=self.hidden, x_dtype=types[x.dtype], y_dtype=self.desc.dtype, h_dtype=self.desc.dtype, scale=scale, eps=self.desc.eps)
         if begin:
             nnv.nnv_residual_norm(desc, rows, x, x.stride(0), None, 0, None, 0, None, 0, None, self.norm_in, None, 0, h, h.stride(0))

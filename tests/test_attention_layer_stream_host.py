@@ -48,7 +48,7 @@ def test_the_attention_that_is_asked_for_runs(calls):
     make().step_stream(x.float(), x, 5, begin=True)
     assert calls[0] == calls[-1] == "nnv_residual_norm" and len(calls) == 7
     del calls[:]
-    make().step_stream(x.float(), x, 5, gate=x, index=torch.zeros(5, dtype=torch.int32))
+    make().step_stream(x.float(), x, 5, gate=x.clone(), index=torch.zeros(5, dtype=torch.int32))
     assert calls[-1] == "nnv_residual_norm" and len(calls) == 6
 
 
@@ -87,6 +87,15 @@ def test_a_stream_that_does_not_fit_is_refused_before_any_call(calls):
     for index in (new(5), torch.zeros(4, dtype=torch.int32), torch.zeros(10, dtype=torch.int32)[::2]):
         with pytest.raises(ValueError):
             layer.step_stream(x, h, 5, gate=new(3, 256), index=index)
+    for gate in (new(4, 256), new(0, 256), new(1, 256).expand(5, 256), new(1281)[1:].view(5, 256)):                # too few, none, no rows of their own, off by two bytes
+        with pytest.raises(ValueError):
+            layer.step_stream(x, h, 5, gate=gate)
+    with pytest.raises(ValueError):
+        layer.step_stream(x, h, 5, scale=float("nan"))
+    both = new(20, 512)
+    for a, b, gate in ((both[:, :256], both[:, 256:], None), (h, h, None), (x, h, h)):                               # in each other's memory
+        with pytest.raises(ValueError):
+            layer.step_stream(a, b, 5, gate=gate)
     with pytest.raises(ValueError):
         layer.step_stream(x, h, 21)
     assert not calls
