@@ -99,20 +99,29 @@ class AttentionLayer:
                              None, self.cache)
 
     def share(self, ends, tokens):
-        """Requests ends[g] to ends[g + 1] - 1 begin with the same tokens[g] tokens (whole blocks), which the first of them holds; the others hold nothing yet, and
-        from here on begin behind them.  No groups: nothing is shared any more by requests that begin later."""
+        """Requests ends[g] to ends[g + 1] - 1 begin with the same tokens[g] tokens (whole blocks), which the first of them holds.  Others that hold nothing yet
+        begin behind them from here on; others that hold something have to run behind these very blocks already, so that groups may be added, taken away and given
+        another first request while they run.  Requests keep the prefix that they began behind whatever is shared later, since its blocks are entered in their own rows of the
+        table: groups say what is read once for all of them.  The first request of a group holds the prefix as long as the group is given: before its place is used again,
+        share without it.  A captured step reads as many groups as there were, of those that there are when it is replayed."""
         ends, tokens, block = list(ends), list(tokens), self.desc.block_tokens
-        held = self.held.tolist()
+        held, table = self.held.tolist(), self.table.cpu()
         if len(tokens) > self.groups or len(ends) != len(tokens) + 1 or sorted(ends) != ends or ends[0] < 0 or ends[-1] > self.requests:
             raise ValueError(f"expected up to {self.groups} groups of the {self.requests} requests, in their order")
+
+        def behind(i, first, n):
+            return held[i] >= n and torch.equal(table[i, : n // block], table[first, : n // block]) and bool((table[i, : n // block] >= 0).all())
+
         for first, end, n in zip(ends, ends[1:], tokens):
-            if n < 0 or n % block or (first < end and held[first] < n) or any(held[i] for i in range(first + 1, end)):
-                raise ValueError(f"{n} tokens: expected whole blocks of {block} that request {first} holds, and nothing held by the others of its group")
+            if n < 0 or n % block or (first < end and held[first] < n) or any(held[i] and not behind(i, first, n) for i in range(first + 1, end)):
+                raise ValueError(f"{n} tokens: expected whole blocks of {block} that request {first} holds, and others of its group that hold nothing or are behind these")
         for first, end, n in zip(ends, ends[1:], tokens):
-            self.held[first + 1:end] = n
-        if tokens:
-            self.group_ends[:len(ends)] = torch.tensor(ends, dtype=torch.int32)
-            self.shared[:len(tokens)] = torch.tensor(tokens, dtype=torch.int32)
+            new = [i for i in range(first + 1, end) if held[i] == 0]
+            self.held[new] = n
+            self.table[new, : n // block] = self.table[first, : n // block]
+        if self.groups:                                      # (behind the last: groups of no request)
+            self.group_ends.copy_(torch.tensor(ends + ends[-1:] * (self.groups - len(tokens)), dtype=torch.int32))
+            self.shared.copy_(torch.tensor(tokens + [0] * (self.groups - len(tokens)), dtype=torch.int32))
         self.n_groups = len(tokens)
 
     def attend(self, rows):
