@@ -266,7 +266,8 @@ __global__ __launch_bounds__(EACH ? 512 : 256, DIM == 256 ? 2 : EACH ? 4 : DIM =
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = a.flip ? -(float)parts[k][e] : (float)parts[k][e];
-                queries[8 * s + e][part][at] = f64x2_t{(double)fmaxf(v, 0.f), (double)fminf(v, 0.f)};
+                const float none = v == v ? 0.f : v;         // (a NaN stays one, and with it the head's sum)
+                queries[8 * s + e][part][at] = f64x2_t{(double)(v > 0 ? v : none), (double)(v < 0 ? v : none)};
             }
         }
     };
