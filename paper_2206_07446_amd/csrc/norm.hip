@@ -81,22 +81,27 @@ template <typename F> __device__ static inline F row_sum(F v, bool alone, F *scr
     return sum;
 }
 
-// 1 / sqrt(mean(v^2) + eps).  Squares that leave float32's range, on either side, are added up again in float64; a row of zeros without eps stays one.
-template <int CHUNKS> __device__ static inline float inverse_rms(const float (&v)[CHUNKS][8], int n, float eps, bool alone, float *scratch, double *scratch_wide) {
+// 1 / sqrt(mean(v^2) + eps).  Squares that leave float32's range, on either side, are added up again in float64; a row of zeros without eps stays one.  Of a row below
+// 2^-128 or so the reciprocal is no float32: it is the product of `factor` and a power of two that moves no bit of v, 1 where the squares are in range.
+struct Inverse { float twos, factor; };
+template <int CHUNKS> __device__ static inline Inverse inverse_rms(const float (&v)[CHUNKS][8], int n, float eps, bool alone, float *scratch, double *scratch_wide) {
     float sum = 0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
     sum = row_sum(sum, alone, scratch);
-    if (sum > 0x1p-80f && sum < INFINITY) return 1.f / sqrtf(sum / (float)n + eps);
+    if (sum > 0x1p-80f && sum < INFINITY) return {1.f, 1.f / sqrtf(sum / (float)n + eps)};
     double wide = 0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) wide += (double)v[c][i] * (double)v[c][i];
     wide = row_sum(wide, alone, scratch_wide) / n + (double)eps;
-    return wide == 0 ? 0.f : (float)(1.0 / sqrt(wide));
+    if (wide == 0) return {1.f, 0.f};
+    const double inverse = 1.0 / sqrt(wide);                 // (twos: not 1 only where what they take off or add lies beyond the range of a result)
+    const float twos = inverse > 0x1p100 ? 0x1p64f : inverse < 0x1p-100 ? 0x1p-64f : 1.f;
+    return {twos, (float)(inverse / (double)twos)};
 }
 
 template <int XT, int YT, bool VEC, int CHUNKS>
@@ -119,11 +124,11 @@ __global__ __launch_bounds__(1024) void residual_norm(ResidualArgs a) {
         if (a.post) {
             float weight[CHUNKS][8];
             at.load(a.post, weight);
-            const float inverse = inverse_rms(y, a.n, a.eps, alone, scratch[0], scratch_wide[0]);
+            const Inverse inverse = inverse_rms(y, a.n, a.eps, alone, scratch[0], scratch_wide[0]);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[c][i] = y[c][i] * inverse * weight[c][i];
+                for (int i = 0; i < 8; ++i) y[c][i] = y[c][i] * inverse.twos * inverse.factor * weight[c][i];
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
@@ -136,11 +141,11 @@ __global__ __launch_bounds__(1024) void residual_norm(ResidualArgs a) {
     }
     if (!a.pre) return;
     at.load(a.pre, w);
-    const float inverse = inverse_rms(r, a.n, a.eps, alone, scratch[1], scratch_wide[1]);
+    const Inverse inverse = inverse_rms(r, a.n, a.eps, alone, scratch[1], scratch_wide[1]);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[c][i] = r[c][i] * inverse * w[c][i];
+        for (int i = 0; i < 8; ++i) r[c][i] = r[c][i] * inverse.twos * inverse.factor * w[c][i];
     const int64_t h = row * a.ldh;
     if (a.h_dtype == NNV_F32) at.store(static_cast<float *>(a.h) + h, r);
     else if (a.h_dtype == NNV_F16) at.store(static_cast<_Float16 *>(a.h) + h, r);
