@@ -9,6 +9,7 @@ stream to the residual stream and the norm for the next layer.
 from __future__ import annotations
 
 import argparse
+import ctypes
 import math
 
 import torch
@@ -16,6 +17,8 @@ import torch
 from . import binding as nnv
 
 DTYPES = {nnv.F16: torch.float16, nnv.BF16: torch.bfloat16}
+NO_TENSORS = -1                # what a call of sizes that it takes returns without tensors (NNV_E_NULL)
+MOST_STREAM = 32768            # values of a row that nnv_residual_norm takes
 
 
 class AttentionLayer:
@@ -29,12 +32,13 @@ class AttentionLayer:
         self.keep, self.first, self.last, self.groups, self.n_groups = keep, first, last, groups, 0
         self.device, self.dtype, self.requests, self.rows, self.hidden = torch.device(device), DTYPES[dtype], requests, rows, hidden
         width = -(-tokens // block_tokens)
-        self.desc = nnv.AttentionDesc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, block_tokens=block_tokens, blocks=requests * width,
-                                      table_blocks=width, rotary_dim=head_dim, rotary_interleaved=0, positions=width * block_tokens, window=window, sinks=sinks, dtype=dtype,
+        self.desc = nnv.AttentionDesc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, block_tokens=block_tokens, blocks=nnv._int(requests * width),
+                                      table_blocks=width, rotary_dim=head_dim, rotary_interleaved=0, positions=nnv._int(width * block_tokens), window=window, sinks=sinks, dtype=dtype,
                                       scale=head_dim ** -0.5, eps=1e-6)
         self.q_size, self.kv_size = q_heads * head_dim, kv_heads * head_dim
         self.qkv_desc = nnv.LinearDesc(n=self.q_size + 2 * self.kv_size, k=hidden, x_dtype=dtype, y_dtype=dtype, raw_dtype=nnv.F32)
         self.out_desc = nnv.LinearDesc(n=hidden, k=self.q_size, x_dtype=dtype, y_dtype=dtype, raw_dtype=nnv.F32)
+        self._fits(nnv._int(rows))
         new = lambda *shape, dtype=self.dtype: torch.empty(*shape, dtype=dtype, device=self.device)  # noqa: E731
         bytes_ = lambda n: new(max(16, n), dtype=torch.uint8)  # noqa: E731
         self.qkv_tx, self.out_tx = (bytes_(nnv.nnv_linear_transformed_bytes(d)) for d in (self.qkv_desc, self.out_desc))
@@ -64,6 +68,24 @@ class AttentionLayer:
         self.table = torch.full((requests, width), -1, dtype=torch.int32, device=self.device)
         self.free = torch.arange(requests * width, dtype=torch.int32, device=self.device)
         self.count = torch.tensor([requests * width], dtype=torch.int32, device=self.device)
+
+    def _fits(self, rows):
+        """Sizes that a call of a step would refuse, after those before it have run, are refused with the layer.  A call looks at its sizes before its tensors, of which there
+        are none here (16: an address that is not looked at), so that it never runs."""
+        lib, desc, step = nnv.load(), ctypes.byref(self.desc), (ctypes.byref(self.desc), self.requests, rows)
+        none = lambda n: (None,) * n  # noqa: E731
+        calls = [("nnv_linear_forward", (ctypes.byref(d), rows, None, d.k, None, None, None, d.n, None, 0, None)) for d in (self.qkv_desc, self.out_desc)]
+        calls += [("nnv_kv_plan", (*step, *none(11))), ("nnv_qk_norm_rope", (desc, rows, 16, self.q_size, None, 0, None, 0, *none(9))), ("nnv_kv_attention", (*step, *none(8), 0, None))]
+        if self.keep:
+            calls += [("nnv_kv_bounds", (*step, *none(6))), ("nnv_kv_select", (*step, self.keep, self.first, self.last, *none(8), 0, None)),
+                      ("nnv_kv_attention_blocks", (*step, self.keep, *none(9), 0, None))]
+        # (what attention over shared prefixes launches goes up and down with the rows; with the groups it goes up, to 64 of them and from there on)
+        if self.groups:
+            calls += [("nnv_kv_attention_shared", (desc, self.requests, m, g, *none(10), 0, None)) for m in range(1, rows + 1) for g in {self.groups, min(self.groups, 64)}]
+        for name, args in calls:
+            status = getattr(lib, name)(*args)
+            if status != NO_TENSORS:
+                raise ValueError(f"{name} does not take {rows} rows of {self.requests} requests of this layer: {nnv.nnv_status_string(status)}")
 
     def _check(self, rows, *tensors):
         """The calls below take addresses: what their buffers do not hold is refused here."""
@@ -161,6 +183,8 @@ class AttentionLayer:
         before left it (begin: the norm of x by norm_in is taken first), after it the norm by norm_next of the new stream.  What is added is the layer's output,
         behind a norm by norm_out where post is set, times scale and its row of gate, or row index[i] of it."""
         self._check(rows, h)
+        if self.hidden > MOST_STREAM:
+            raise ValueError(f"a stream has at most {MOST_STREAM} values a row")
         types = {torch.float32: nnv.F32, torch.float16: nnv.F16, torch.bfloat16: nnv.BF16}
         if not (isinstance(x, torch.Tensor) and x.dtype in types and x.device == self.qkv.device and x.dim() == 2 and x.shape[0] >= rows and x.shape[1] == self.hidden
                 and x.stride(1) == 1 and (rows <= 1 or x.stride(0) >= self.hidden) and x.data_ptr() % 16 == 0):
