@@ -181,7 +181,8 @@ class AttentionLayer:
     def step_stream(self, x, h, rows, begin=False, post=False, gate=None, index=None, scale=1.0):
         """A step on the residual stream x (rows of float32 or 16 bits, updated in place).  h: rows of the layer's type, in it this layer's input as the layer
         before left it (begin: the norm of x by norm_in is taken first), after it the norm by norm_next of the new stream.  What is added is the layer's output,
-        behind a norm by norm_out where post is set, times scale and its row of gate, or row index[i] of it."""
+        behind a norm by norm_out where post is set, times scale and its row of gate, or row index[i] of it.  x and h lie apart from each other and the others, each from the
+        first of its rows to the last: not as columns of one buffer."""
         self._check(rows, h)
         if self.hidden > MOST_STREAM:
             raise ValueError(f"a stream has at most {MOST_STREAM} values a row")
@@ -198,9 +199,14 @@ class AttentionLayer:
             raise ValueError("expected a finite scale")
         if index is not None and not (isinstance(index, torch.Tensor) and index.dtype == torch.int32 and index.device == self.qkv.device and index.is_contiguous() and index.numel() >= rows):
             raise ValueError(f"expected {rows} int32 or more on {self.qkv.device}")
-        memory = [t.untyped_storage().data_ptr() for t in (x, h, gate, index) if t is not None]      # (what is written, first)
-        if rows and (memory[0] in memory[1:] or memory[1] in memory[2:]):
-            raise ValueError("expected the stream and the norms in memory of their own")
+        # from the first byte to the last of what is written, and of what is read beside it
+        span = lambda t, values: (t.data_ptr(), t.data_ptr() + values * t.element_size())  # noqa: E731
+        matrix = lambda t, m: span(t, (m - 1) * t.stride(0) + self.hidden)  # noqa: E731
+        written, read = [matrix(x, rows), matrix(h, rows)], [matrix(self.out, rows)]
+        if gate is not None:
+            read += [matrix(gate, gates)] + ([] if index is None else [span(index, rows)])
+        if rows and any(a < end and first < b for i, (a, b) in enumerate(written) for first, end in written[:i] + read):
+            raise ValueError("expected the stream and the norms apart from each other, from gates and indices and from the layer's own rows")
         desc = nnv.ResidualDesc(n=self.hidden, x_dtype=types[x.dtype], y_dtype=self.desc.dtype, h_dtype=self.desc.dtype, scale=scale, eps=self.desc.eps)
         if begin:
             nnv.nnv_residual_norm(desc, rows, x, x.stride(0), None, 0, None, 0, None, 0, None, self.norm_in, None, 0, h, h.stride(0))
