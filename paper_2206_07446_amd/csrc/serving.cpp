@@ -364,10 +364,9 @@ int nnv_residual_norm(const nnv_residual_desc *desc, int m, const void *x, int64
     if (!pre) h = nullptr;
     if (!gate) index = nullptr;
     if (gate && (gates < 1 || (!index && gates != 1 && gates < m))) return NNV_E_ARG;
-    if (m > 1 && (ldx < n || (y && (ldy < n || ldo < n)) || (pre && ldh < n))) return NNV_E_ARG;
-    if (gate && gates > 1 && ldg < n) return NNV_E_ARG;
-    for (int64_t ld : {ldx, ldy, ldg, ldo, ldh})
-        if (ld > kMostStride) return NNV_E_ARG;
+    auto apart = [&](int64_t ld) { return ld >= n && ld <= kMostStride; };
+    if (m > 1 && (!apart(ldx) || (y && (!apart(ldy) || !apart(ldo))) || (pre && !apart(ldh)))) return NNV_E_ARG;
+    if (gate && gates > 1 && !apart(ldg)) return NNV_E_ARG;
     if (off16(x) || off16(y) || off16(post) || off16(gate) || off4(index) || off16(pre) || off16(x_out) || off16(h)) return NNV_E_ALIGN;
     const int xb = element_bytes(desc->x_dtype), yb = element_bytes(desc->y_dtype), hb = element_bytes(desc->h_dtype);
     auto step = [&](int64_t ld, int bytes) { return m > 1 ? ld * bytes : 0; };
