@@ -434,11 +434,11 @@ int nnv_kv_bounds(const nnv_attention_desc *desc, int n_requests, int n_rows, co
 /* The blocks that rows select, by place in their request (token / block_tokens): of those that a row sees (the blocks of tokens j <= p, j < lengths[i])
  * the first n_first and the last n_last, and of the others those of the largest scores, `keep` in all or as many as there are.  The score is the
  * largest, over the query heads that read key head h, of the sum over d of max(q[d] hi[d], q[d] lo[d]) (with -q in the place of q where desc.scale is negative), in float64;
- * equal ones go to the lower block, sums that are no number count as -infinity.  Products of a query's 8 or 11 bits with a bound's 2 are exact there, and
+ * equal ones go to the lower block, sums that are no number (a head that holds a NaN) count as -infinity.  Products of a query's 8 or 11 bits with a bound's 2 are exact there, and
  * so are sums whose terms span fewer than 2^32: then the selection depends on no order.
  *   selected : n_rows x kv_heads x keep int32, ascending, -1 behind the last (and in rows that see nothing)
  *   workspace : >= nnv_kv_select_workspace_bytes(desc, n_requests, n_rows) bytes, whatever its contents
- * 1 <= keep <= 2^20, n_first, n_last >= 0, n_first + n_last <= keep; at most 32768 table_blocks (UNSUPPORTED).  Blocks whose table entry is none of the cache are not selected.
+ * 1 <= keep <= 2^20, n_first, n_last >= 0, n_first + n_last <= keep; fewer than 2^22 rows and requests times kv_heads (ARG); at most 32768 table_blocks (UNSUPPORTED).  Blocks whose table entry is none of the cache are not selected.
  * Errors: NULL, BAD_DESC, UNSUPPORTED, ARG, WORKSPACE, ALIGN, HIP. */
 size_t nnv_kv_select_workspace_bytes(const nnv_attention_desc *desc, int n_requests, int n_rows);
 int nnv_kv_select(const nnv_attention_desc *desc, int n_requests, int n_rows, int keep, int n_first, int n_last, const void *q, const int32_t *block_table,

@@ -192,7 +192,8 @@ template <int R, int SEEN> __device__ static inline Tile find_tile(const AttendA
 struct Part { Tile tile; int split, splits; };
 
 // Part u of a key head.  Groups differ in rows and in prefixes: their tiles are cut so that parts have as many steps of S tokens each (a.prefix_units of them in all
-// and one more of each tile at most), which every wavefront works out by itself, a lane to a group.  More than 64 groups have tiles enough, cut alike.
+// and one more of each tile at most), which every wavefront works out by itself, a lane to a group.  More than 64 groups have tiles enough, cut alike (200 requests behind 4000 tokens: 64
+// groups 64.6 us, 65 64.7; behind 900 37.3, 38.0).
 template <int R, int S> __device__ static inline Part find_part(const AttendArgs &a, int u) {
     if (a.n_groups > 64) return {find_tile<R, kPrefix>(a, u / a.prefix_splits, nullptr), u % a.prefix_splits, a.prefix_splits};
     const int lane = threadIdx.x & 63;
@@ -207,10 +208,12 @@ template <int R, int S> __device__ static inline Part find_part(const AttendArgs
     // (each tile's last part counts as one more; rounded up by more than the sum is off: no more parts than there are workgroups)
     const float units = fmaxf(a.prefix_units - whole, 0.5f * a.prefix_units);
     int each = max(a.prefix_least, (int)fminf(ceilf(total * 1.001f / units), 1e9f));
-    // (where that would be less than prefix_short, two thirds of the parts: what a part costs beside its steps is then most of it)
+    // (where that would be less than prefix_short, two thirds of the parts: what a part costs beside its steps is then most of it.  192 requests behind 2400 tokens 47.6 us, with
+    // all parts 51.1; 64 behind 4800 30.7, 32.1; 16 behind 9600 21.5, 22.7; of 18 such sizes the others alike)
     auto shortest_of = [&](float length) { return length < a.prefix_short ? min(max((int)ceilf(length * 1.5f), a.prefix_least), a.prefix_short) : (int)fminf(ceilf(length), 1e9f); };
     if (a.n_groups <= 16) {
-        // of 64 lengths from the shortest that could do, a lane each, the first that gives no more parts than that
+        // of 64 lengths from the shortest that could do, a lane each, the first that gives no more parts than that.  (128 requests, 8000 tokens: 16 groups 65.9 us, with
+        // the bound above 67.9, 5 groups 51.5, 50.3; 24 groups 75.0 so, 78.0, but behind 1000 tokens 29.7, 27.6, and 64 groups 95.8, 91.9: the loop over the groups)
         const int shortest = max(a.prefix_least, shortest_of(total / a.prefix_units)), tried = shortest + lane * ((shortest + 63) / 64);
         float parts = 0;
         for (int g = 0; g < a.n_groups; ++g)
@@ -1006,9 +1009,10 @@ __global__ __launch_bounds__(256, DIM == 256 ? 1 : DIM == 128 ? 2 : 3) void kv_a
 
 // Prefixes and what requests have behind them in one launch: the workgroups of prefixes first, which take longest; while they keep the matrix cores busy, the
 // others read.  softmax over the tokens of both is that of two softmaxes with bases and sums of their own, which the join brings to one base.  MANY: prefixes by 128 pairs.
-// (64 requests of up to 1024 tokens behind 8192, 32 heads of 128: prefixes by themselves 23 us, the others 17.5, in one launch 33; a launch each 49.  96 requests of
-// 15 pairs behind five prefixes: 121 us, vector instructions 49 % of a compute unit's busy time, matrix ones 34 %: of 128 pairs of a tile 104 are there on
-// average.  7 requests of 4 pairs: 9 us, a chain of loads.)  With the longest of the others first, or all of them before the prefixes, it takes as long or longer (43, 43 us).
+// (64 requests of up to 1024 tokens behind 8192, 32 heads of 128: the call 41-42 us, with a launch each 48; traced 37 and the join 6, prefixes by themselves 23, the others 17.5.
+// 96 requests of 15 pairs behind five prefixes: the call 115 us, with a launch each 140; traced 121 and the join 9, vector instructions 49 % of a compute unit's busy time, matrix ones 34 %: of 128
+// pairs of a tile 104 are there on average.  7 requests of 4 pairs: the call 11.7 us, traced 8.4 and 3.1, a chain of loads.)  With the longest of the others first, or all of
+// them before the prefixes, the first of these calls takes as long or longer (43, 43 us).
 template <int DT, int DIM, bool MANY>
 __global__ __launch_bounds__(256, MANY ? (DIM == 256 ? 1 : DIM == 128 ? 2 : 3) : DIM == 256 ? 2 : 4) void kv_attend_shared(AttendArgs a) {
     __shared__ union Lds {
@@ -1292,7 +1296,7 @@ static SharedSizes shared_sizes(const nnv_attention_desc &d, int requests, int r
     const bool own_many = attend_many(d, requests, rows) && pairs >= (int64_t)2 * kManyPairs * requests;      // (of fewer on average, nearly all are few)
     SharedSizes s{};
     s.many = own_many || pairs >= (int64_t)kManyPairs * groups;
-    auto within = [&](int64_t splits, int64_t most) {     // of memory, and of what the join takes
+    auto within = [&](int64_t splits, int64_t most) {     // of memory (one result each of a prefix and behind it there is at least, whatever these take), and of what the join takes
         splits = splits < most ? splits : most;
         splits = splits < kMostSplits ? splits : kMostSplits;
         while (splits > 1 && splits * each > (int64_t)128 << 20) splits = splits / 2;
@@ -1377,6 +1381,7 @@ template <int DT, int DIM> static hipError_t launch_shared_dim(const nnv_attenti
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int all = a.rows * a.q_heads;
+    // (behind 4096 tokens, by wavefronts and by workgroups: 8192 rows and heads 64.2 us, 67.7; 4096 42.7, 43.8; 2048 30.9, 30.8; 256 16.5, 16.4)
     if (all >= 4096) kv_attend_join_rows<DT, DIM><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a, all);
     else kv_attend_join_shared<DT, DIM><<<(unsigned)all, 256, 0, st>>>(a);
     return hipGetLastError();
