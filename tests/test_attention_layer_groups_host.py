@@ -63,3 +63,18 @@ def test_layers_without_groups_share_nothing(monkeypatch):
         monkeypatch.setattr(nnv.binding, name, lambda *a, name=name: names.append(name))
     layer.attend(3)
     assert names == ["nnv_kv_attention"]
+
+
+def test_the_first_request_of_a_group_may_end():
+    """Its place is used again: the group is refused as it was, and given with another that runs behind the same blocks."""
+    layer = running()
+    layer.share([0, 3], [32])
+    layer.held[0] = 0
+    with pytest.raises(ValueError):
+        layer.share([0, 3], [32])
+    layer.held[0], layer.table[0, :3] = 40, torch.tensor([1, 4, 6], dtype=torch.int32)
+    with pytest.raises(ValueError):
+        layer.share([0, 3], [32])
+    layer.share([1, 3], [32])
+    assert layer.group_ends.tolist() == [1, 3, 3] and layer.held.tolist() == [40, 32, 32, 20, 0, 0]
+    assert layer.table[:3, :3].tolist() == [[1, 4, 6], [5, 9, -1], [5, 9, -1]]
